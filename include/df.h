@@ -299,6 +299,110 @@ typedef struct df_pack_args {
 
 df_status df_pack_context(const df_pack_args *args, void *stream);
 
+/* ------------------------------------------------------------------------
+ * A paged cache: the per-head sink + ring cache of a BATCH of requests (videos, token streams), in pages that are
+ * handed out on the device.  Everything that changes from step to step - lengths, block tables, the stack of free
+ * pages - lies in device memory: nothing is copied to the host, and a captured graph stays valid while requests grow,
+ * end and are replaced.
+ *
+ * A page holds page_tokens rows of ONE key head, so a head owns pages only for what it keeps.  Key head h of request b
+ * keeps the request's first sink_cap tokens and the win_cap most recent later ones (a head that keeps every token has
+ * a window no request reaches; a dummy head has both 0 and owns no page).  Position j of the request has the slot
+ *     j                                     if j < sink_cap,
+ *     sink_cap + (j - sink_cap) % win_cap   otherwise,
+ * slot r lies in page block_table[b][h][r / page_tokens], row r % page_tokens, and the first
+ * min(len[b], sink_cap + win_cap) slots are filled.
+ *
+ * The device arrays are checked on the device: lengths, offsets and page numbers out of range read and write nothing
+ * outside the buffers.  df_page_map reports them, df_paged_append skips such rows, and in df_paged_attn the rows of a
+ * request's head whose pages are not pages of the pool come out as NaN.
+ * ---------------------------------------------------------------------- */
+enum { DF_BF16 = 0, DF_FP16 = 1 };
+
+typedef struct df_paged_cache {
+  void *k_pages, *v_pages;     /* DEVICE [n_pages, page_tokens, d] of dtype, 16-byte aligned                     */
+  int32_t *block_table;        /* DEVICE [B, H_kv, max_pages]; entries of pages not held have no meaning         */
+  const int32_t *len;          /* DEVICE [B] tokens of the request that the cache has taken, kept or not (< 2^30) */
+  const int32_t *sink_cap;     /* DEVICE, head h of request b at [b*cap_stride + h], 0 <= . <= 2^30              */
+  const int32_t *win_cap;      /* DEVICE, same layout                                                            */
+  int64_t cap_stride;          /* H_kv, or 0 where all requests have the same heads                              */
+  int32_t *free_pages;         /* DEVICE [n_pages]: the first *n_free are free, the last of them is taken next   */
+  const int32_t *n_free;       /* DEVICE [1]                                                                     */
+  int32_t B, H_kv, d, dtype;   /* requests, key heads (<= DF_MAX_HEADS), head dim (64 or 128), DF_BF16 or DF_FP16 */
+  int32_t n_pages, page_tokens, max_pages; /* pages of the pool, tokens of a page (16, 32, ... 1024), width of the table */
+} df_paged_cache;
+
+/* df_page_map: make room for the new tokens of every request, and say where they go.  Request b has the new tokens
+ * cu_new[b] .. cu_new[b+1]-1 of the packed batch (cu_new[0] >= 0, not falling, cu_new[B] <= total_new); its positions
+ * len[b], len[b]+1, ...  Pages are taken from the free stack in the order of (request, head, page), the stack's last
+ * first.  release[b] != 0: request b has ended; its pages go back to the stack first (same order), and its new
+ * tokens, if any, are those of another request that begins at position 0.
+ * slot_map[t][h] = page * page_tokens + row for token t of the packed batch, or -1 where head h does not keep it (of
+ * a chunk longer than the window only the last win_cap tokens are kept) and for tokens of no request.
+ * All or nothing: *status is DF_OK, or DF_ERR_RANGE where the stack has too few pages, a head needs more than
+ * max_pages, or a device array is out of range; then the table, the stack, len_out and n_free_out are as before the
+ * call (len_out = len, n_free_out = *n_free) and the slot map is -1 throughout.
+ * The cache's len and n_free are read; the new ones go to len_out and n_free_out, which may be the same arrays.
+ * Launches: one kernel, two from 8192 slots on. */
+typedef struct df_page_map_args {
+  const df_paged_cache *cache;
+  const int32_t *cu_new;       /* DEVICE [B+1]                                     */
+  const uint8_t *release;      /* DEVICE [B] or NULL (none has ended)              */
+  int64_t *slot_map;           /* DEVICE out [total_new, H_kv]                     */
+  int32_t *len_out;            /* DEVICE out [B]                                   */
+  int32_t *n_free_out;         /* DEVICE out [1]                                   */
+  int32_t *status;             /* DEVICE out [1]                                   */
+  int32_t total_new;           /* rows of slot_map (>= 0; 0: releases only)        */
+} df_page_map_args;
+
+df_status df_page_map(const df_page_map_args *args, void *stream);
+
+/* df_paged_append: row slot_map[t][h] of the pool = key (value) of token t, head h; entries that are no slot of the
+ * pool (-1) are skipped and cost no traffic.  Launches: one kernel. */
+typedef struct df_paged_append_args {
+  const df_paged_cache *cache;
+  const void *k_new;           /* DEVICE, (t,h,c) at k_new[t*stride_tok + h*stride_head + c] */
+  const void *v_new;
+  int64_t stride_tok, stride_head;
+  const int64_t *slot_map;     /* DEVICE [total_new, H_kv] */
+  int32_t total_new;
+} df_paged_append_args;
+
+df_status df_paged_append(const df_paged_append_args *args, void *stream);
+
+/* df_paged_attn: attention of the new tokens of every request over its cache and over themselves, one call for the
+ * batch; the new tokens' keys need not be in the cache (as for df_attn_fwd they come beside it and may change from
+ * denoising step to denoising step), so the call goes before the append of the same tokens.
+ * Query i of request b (row cu_new[b] + i) belongs to the causal block of new tokens first .. last-1 with
+ * first = (i / block) * block, last = min(first + block, n_b), and sees
+ *     the kept position j < len[b]  if  j < sink_cap  or  j >= len[b] + first - win_cap,
+ *     the new token t               if  t < last  and  (t >= first - win_cap  or  len[b] + t < sink_cap).
+ * block = 1: token by token; block = tokens of a frame: frame by frame; block >= n_b: every new token sees all.
+ * Query head g reads key head g / (H_q / H_kv).  out = softmax(scale * q k) v over what is seen; a row that sees
+ * nothing (k_cur NULL and no history), or only keys that score minus infinity, is 0 with a log-sum-exp of minus
+ * infinity.  What a row does not see has no influence on it, whatever its value, NaN included.  Rows of no request
+ * (before cu_new[0], behind cu_new[B]) are left as they were.
+ * Launches: one kernel, and a second one that puts split units together unless no unit can be long enough to be
+ * split.  Nothing waits on the device, nothing in the workspace has to be cleared, and results do not change from
+ * call to call.  Two calls that use the same workspace must not overlap on the device. */
+typedef struct df_paged_attn_args {
+  const df_paged_cache *cache; /* free_pages and n_free are not used and may be NULL */
+  const void *q;  int64_t q_stride_tok, q_stride_head;          /* DEVICE [total_new, H_q, d]               */
+  const void *k_cur, *v_cur; int64_t kc_stride_tok, kc_stride_head; /* DEVICE [total_new, H_kv, d]; both NULL: the new
+                                                                   tokens only look back                    */
+  const int32_t *cu_new;       /* DEVICE [B+1], as in df_page_map_args                                      */
+  void *out; int64_t o_stride_tok, o_stride_head;               /* DEVICE [total_new, H_q, d]               */
+  float *lse_out;              /* DEVICE fp32 [H_q, total_new] natural-log sum-exp of the scaled logits, or NULL */
+  int32_t H_q, total_new;      /* query heads (a multiple of H_kv, at most 64 times as many), rows of q     */
+  int32_t max_new;             /* 1 <= . <= total_new, at least every n_b: a request's tokens beyond it are left out */
+  int32_t block;               /* tokens of a causal block, > 0                                             */
+  float softmax_scale;         /* positive and finite                                                       */
+  void *workspace; size_t workspace_bytes; /* DEVICE, >= df_paged_workspace_bytes(...), 256-byte aligned; scratch */
+} df_paged_attn_args;
+
+size_t df_paged_workspace_bytes(int32_t H_q, int32_t H_kv, int32_t d, int32_t max_new);
+df_status df_paged_attn(const df_paged_attn_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,9 +25,11 @@ DF_OK = 0
 DF_MAX_HEADS = 64
 DF_HEAD_FULL, DF_HEAD_SINK, DF_HEAD_NEIGHBOR, DF_HEAD_DUMMY, DF_HEAD_PACK_DUMMY = range(5)
 DF_CLASSIFY_TWO_CLASS, DF_CLASSIFY_DHP = 0, 1
+DF_BF16, DF_FP16 = 0, 1
 
 EXPORTS = ["df_status_string", "df_head_context", "df_attn_workspace_bytes", "df_attn_fwd", "df_attn_fwd_static", "df_attn_plan", "df_attn_units",
-           "df_head_score", "df_classify", "df_kv_append", "df_pack_context"]
+           "df_head_score", "df_classify", "df_kv_append", "df_pack_context",
+           "df_page_map", "df_paged_append", "df_paged_workspace_bytes", "df_paged_attn"]
 
 
 class DfError(RuntimeError):
@@ -93,6 +95,34 @@ class df_pack_args(C.Structure):
                 ("hist_off_out", C.POINTER(C.c_int64)), ("sink_len_out", C.POINTER(C.c_int32))]
 
 
+class df_paged_cache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("block_table", C.c_void_p), ("len", C.c_void_p),
+                ("sink_cap", C.c_void_p), ("win_cap", C.c_void_p), ("cap_stride", C.c_int64),
+                ("free_pages", C.c_void_p), ("n_free", C.c_void_p),
+                ("B", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32),
+                ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class df_page_map_args(C.Structure):
+    _fields_ = [("cache", C.POINTER(df_paged_cache)), ("cu_new", C.c_void_p), ("release", C.c_void_p), ("slot_map", C.c_void_p),
+                ("len_out", C.c_void_p), ("n_free_out", C.c_void_p), ("status", C.c_void_p), ("total_new", C.c_int32)]
+
+
+class df_paged_append_args(C.Structure):
+    _fields_ = [("cache", C.POINTER(df_paged_cache)), ("k_new", C.c_void_p), ("v_new", C.c_void_p),
+                ("stride_tok", C.c_int64), ("stride_head", C.c_int64), ("slot_map", C.c_void_p), ("total_new", C.c_int32)]
+
+
+class df_paged_attn_args(C.Structure):
+    _fields_ = [("cache", C.POINTER(df_paged_cache)),
+                ("q", C.c_void_p), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("k_cur", C.c_void_p), ("v_cur", C.c_void_p), ("kc_stride_tok", C.c_int64), ("kc_stride_head", C.c_int64),
+                ("cu_new", C.c_void_p),
+                ("out", C.c_void_p), ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64),
+                ("lse_out", C.c_void_p), ("H_q", C.c_int32), ("total_new", C.c_int32), ("max_new", C.c_int32), ("block", C.c_int32),
+                ("softmax_scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with __graft_entry__.build() "
@@ -124,6 +154,14 @@ def _load() -> C.CDLL:
     lib.df_kv_append.argtypes = [C.POINTER(df_append_args), C.c_void_p]
     lib.df_pack_context.restype = C.c_int32
     lib.df_pack_context.argtypes = [C.POINTER(df_pack_args), C.c_void_p]
+    lib.df_page_map.restype = C.c_int32
+    lib.df_page_map.argtypes = [C.POINTER(df_page_map_args), C.c_void_p]
+    lib.df_paged_append.restype = C.c_int32
+    lib.df_paged_append.argtypes = [C.POINTER(df_paged_append_args), C.c_void_p]
+    lib.df_paged_workspace_bytes.restype = C.c_size_t
+    lib.df_paged_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+    lib.df_paged_attn.restype = C.c_int32
+    lib.df_paged_attn.argtypes = [C.POINTER(df_paged_attn_args), C.c_void_p]
     return lib
 
 
@@ -412,3 +450,123 @@ def prepared_append(cache: Cache, k_new, v_new, stream=None):
     def call(_keep=keep):
         _check(lib.df_kv_append(C.byref(a), handle), "df_kv_append")
     return call
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _like(t, dtype, shape, device, what: str):
+    """A device array of the paged cache: the library takes it by address alone, so type, shape and place are looked at here."""
+    _want(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.device == device,
+          f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+class PagedCache:
+    """Pages, block tables, lengths and free pages of a batch of requests (df_paged_cache), all of them device tensors of the caller:
+    k_pages, v_pages [n_pages, page_tokens, d] bf16 or fp16; block_table [B, H_kv, max_pages], length [B], free_pages [n_pages],
+    n_free [1] int32; sink_cap, win_cap int32 [H_kv], or [B, H_kv] where requests have heads of their own."""
+
+    def __init__(self, k_pages, v_pages, block_table, length, sink_cap, win_cap, free_pages, n_free):
+        import torch
+        i32, dev = torch.int32, k_pages.device
+        _want(k_pages.dim() == 3 and block_table.dim() == 3, "k_pages and block_table have three dimensions")
+        _want(k_pages.dtype in (torch.bfloat16, torch.float16), f"pages are bf16 or fp16, not {k_pages.dtype}")
+        n_pages, page_tokens, d = k_pages.shape
+        B, H, max_pages = block_table.shape
+        for pages, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            _like(pages, k_pages.dtype, (n_pages, page_tokens, d), dev, what)
+        _like(block_table, i32, (B, H, max_pages), dev, "block_table")
+        _like(length, i32, (B,), dev, "length")
+        per_request = sink_cap.dim() == 2
+        for cap, what in ((sink_cap, "sink_cap"), (win_cap, "win_cap")):
+            _like(cap, i32, (B, H) if per_request else (H,), dev, what)
+        _like(free_pages, i32, (n_pages,), dev, "free_pages")
+        _like(n_free, i32, (1,), dev, "n_free")
+        self.k_pages, self.v_pages, self.block_table, self.length = k_pages, v_pages, block_table, length
+        self.sink_cap, self.win_cap, self.free_pages, self.n_free = sink_cap, win_cap, free_pages, n_free
+        self.c = df_paged_cache()
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages), ("block_table", block_table), ("len", length), ("sink_cap", sink_cap),
+                        ("win_cap", win_cap), ("free_pages", free_pages), ("n_free", n_free)):
+            setattr(self.c, name, _ptr(t))
+        self.c.cap_stride = H if per_request else 0
+        self.c.B, self.c.H_kv, self.c.d = B, H, d
+        self.c.dtype = DF_BF16 if k_pages.dtype == torch.bfloat16 else DF_FP16
+        self.c.n_pages, self.c.page_tokens, self.c.max_pages = n_pages, page_tokens, max_pages
+        self.B, self.Hkv, self.d, self.dtype, self.device = B, H, d, k_pages.dtype, dev
+        self._i32, self._i64, self._u8, self._f32 = torch.int32, torch.int64, torch.uint8, torch.float32
+        self.ref = C.pointer(self.c)
+
+    def _rows(self, t, heads: int, what: str):
+        """[tokens, heads, d] in any token and head strides, d contiguous; strides of dimensions of one do not matter."""
+        _want(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.d and t.dtype == self.dtype and t.device == self.device,
+              f"{what}: [tokens, {heads}, {self.d}] {self.dtype} on {self.device} is needed, not {tuple(t.shape)} {t.dtype} on {t.device}")
+        tok, head, one = t.stride()
+        _want(one == 1, f"{what}: the head dimension has to be contiguous")
+        return (tok if t.shape[0] > 1 else heads * self.d), (head if heads > 1 else self.d)
+
+
+def df_page_map(cache: PagedCache, cu_new, slot_map, status, release=None, len_out=None, n_free_out=None, stream=None):
+    """cu_new [B+1] int32, slot_map [total, H_kv] int64, status [1] int32, release [B] uint8 or None; len_out and n_free_out are the
+    cache's own length and n_free where they are not given."""
+    dev = cache.device
+    _like(cu_new, cache._i32, (cache.B + 1,), dev, "cu_new")
+    _like(slot_map, cache._i64, (slot_map.shape[0], cache.Hkv), dev, "slot_map")
+    _like(status, cache._i32, (1,), dev, "status")
+    len_out = cache.length if len_out is None else len_out
+    n_free_out = cache.n_free if n_free_out is None else n_free_out
+    _like(len_out, cache._i32, (cache.B,), dev, "len_out")
+    _like(n_free_out, cache._i32, (1,), dev, "n_free_out")
+    if release is not None:
+        _like(release, cache._u8, (cache.B,), dev, "release")
+    a = df_page_map_args()
+    a.cache = cache.ref
+    a.cu_new, a.release, a.slot_map = _ptr(cu_new), _ptr(release), _ptr(slot_map)
+    a.len_out, a.n_free_out, a.status, a.total_new = _ptr(len_out), _ptr(n_free_out), _ptr(status), slot_map.shape[0]
+    _check(lib.df_page_map(C.byref(a), _stream_handle(stream)), "df_page_map")
+
+
+def df_paged_append(cache: PagedCache, k_new, v_new, slot_map, stream=None):
+    """k_new, v_new [total, H_kv, d] (any token and head strides), slot_map [total, H_kv] int64 from df_page_map."""
+    tok, head = cache._rows(k_new, cache.Hkv, "k_new")
+    _want(cache._rows(v_new, cache.Hkv, "v_new") == (tok, head) and v_new.shape == k_new.shape, "v_new: not laid out as k_new")
+    _like(slot_map, cache._i64, (k_new.shape[0], cache.Hkv), cache.device, "slot_map")
+    a = df_paged_append_args()
+    a.cache = cache.ref
+    a.k_new, a.v_new, a.slot_map = _ptr(k_new), _ptr(v_new), _ptr(slot_map)
+    a.stride_tok, a.stride_head, a.total_new = tok, head, k_new.shape[0]
+    _check(lib.df_paged_append(C.byref(a), _stream_handle(stream)), "df_paged_append")
+
+
+def df_paged_workspace_bytes(H_q: int, H_kv: int, d: int, max_new: int) -> int:
+    return int(lib.df_paged_workspace_bytes(H_q, H_kv, d, max_new))
+
+
+def df_paged_attn(q, k_cur, v_cur, cache: PagedCache, cu_new, out, softmax_scale, block=1, max_new=None, lse_out=None, workspace=None,
+                  stream=None):
+    """q, out [total, H_q, d], k_cur, v_cur [total, H_kv, d] (any token and head strides) or both None; cu_new [B+1] int32; lse_out
+    [H_q, total] fp32.  block: tokens of a causal block (1: token by token; at least the longest request's: all see all); max_new: the
+    most new tokens that a request has (default: all of them)."""
+    H_q, total = q.shape[1], q.shape[0]
+    a = df_paged_attn_args()
+    a.cache = cache.ref
+    a.q, a.out = _ptr(q), _ptr(out)
+    a.q_stride_tok, a.q_stride_head = cache._rows(q, H_q, "q")
+    a.o_stride_tok, a.o_stride_head = cache._rows(out, H_q, "out")
+    _want(out.shape == q.shape, "out: not as many rows as q")
+    if k_cur is not None or v_cur is not None:
+        _want(k_cur is not None and v_cur is not None, "k_cur and v_cur come together")
+        a.kc_stride_tok, a.kc_stride_head = cache._rows(k_cur, cache.Hkv, "k_cur")
+        _want(k_cur.shape[0] == total, "k_cur: not as many rows as q")
+        _want(cache._rows(v_cur, cache.Hkv, "v_cur") == (a.kc_stride_tok, a.kc_stride_head) and v_cur.shape == k_cur.shape,
+              "v_cur: not laid out as k_cur")
+        a.k_cur, a.v_cur = _ptr(k_cur), _ptr(v_cur)
+    _like(cu_new, cache._i32, (cache.B + 1,), cache.device, "cu_new")
+    if lse_out is not None:
+        _like(lse_out, cache._f32, (H_q, total), cache.device, "lse_out")
+    a.cu_new, a.lse_out = _ptr(cu_new), _ptr(lse_out)
+    a.H_q, a.total_new, a.max_new, a.block, a.softmax_scale = H_q, total, total if max_new is None else max_new, block, softmax_scale
+    a.workspace = _ptr(workspace)
+    a.workspace_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(lib.df_paged_attn(C.byref(a), _stream_handle(stream)), "df_paged_attn")

@@ -13,7 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdf_hip.so")
 MARSHAL = os.path.join(PKG, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # for this interpreter alone
-SOURCES = ["df_host.cpp", "df_cache.hip", "df_attn.hip"]
+SOURCES = ["df_host.cpp", "df_cache.hip", "df_attn.hip", "df_paged.hip", "df_paged_attn.hip"]
 
 
 def hipcc_command(out: str = LIB, extra=()):

@@ -1,0 +1,38 @@
+// What the paged cache's translation units share: the slots of a head, and the host's checks of a df_paged_cache.
+#pragma once
+
+#include "df_internal.h"
+
+namespace df {
+
+constexpr int kMaxLen = 1 << 30;       // bound of lengths, sinks and windows
+
+__host__ __device__ inline int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Filled slots after `len` tokens: min(len, sink + win), whose sum may not fit into 32 bits.
+__host__ __device__ inline int filled_slots(int len, int sink, int win) {
+  return len < sink || len - sink < win ? len : sink + win;
+}
+
+// Slot of position j in a head with a window, and of a sink position in any.
+__host__ __device__ inline int slot_of(int j, int sink, int win) { return j < sink ? j : sink + (j - sink) % win; }
+
+inline int log2_of(int x) {
+  int n = 0;
+  while ((1 << n) < x) ++n;
+  return n;
+}
+
+inline df_status check_paged_cache(const df_paged_cache *c) {
+  if (!c) return DF_ERR_NULL;
+  if (c->B <= 0 || c->H_kv <= 0 || c->n_pages <= 0 || c->max_pages <= 0 || c->page_tokens <= 0) return DF_ERR_SHAPE;
+  if (c->H_kv > kMaxHeads || (c->d != 64 && c->d != 128) || (c->dtype != DF_BF16 && c->dtype != DF_FP16)) return DF_ERR_UNSUPPORTED;
+  if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1))) return DF_ERR_UNSUPPORTED;
+  if (c->B > (1 << 16) || c->n_pages > kMaxLen || c->max_pages > kMaxLen) return DF_ERR_RANGE;
+  if (!c->k_pages || !c->v_pages || !c->block_table || !c->len || !c->sink_cap || !c->win_cap) return DF_ERR_NULL;
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages)) return DF_ERR_ALIGN;
+  if (c->cap_stride != 0 && c->cap_stride < c->H_kv) return DF_ERR_SHAPE;
+  return DF_OK;
+}
+
+}  // namespace df

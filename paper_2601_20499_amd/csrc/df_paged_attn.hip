@@ -1,0 +1,1027 @@
+// df_paged_attn: attention of the new tokens of a batch of requests over paged caches and over themselves.
+//
+// Mathematics.  Per row out = sum_k 2^(c s_k - c m) v_k / sum_k 2^(c s_k - c m), c = scale log2(e), in one pass over the keys: m
+// is a reference that follows the running maximum of s, and sum and output are rescaled where it moves.  Sums, maxima and
+// outputs are held in 32 bits; the weights are rounded to the tensors' type for the second product (the matrix core takes both
+// operands in 16 bits), the sum takes them unrounded.
+//
+// Layout.  The query heads of a key head are taken together: row r of a (request, key head) is query r / G of head
+// r % G, so the keys are read once for all of them and a single token of G heads is one tile of rows.  Scores are
+// computed transposed, S^T = K Q^T with v_mfma_f32_16x16x32: a lane owns one row (lane % 16) and, because the rows of K are
+// dealt to the operand's rows as key_of_operand_row says, its scores are already the second product's operand P^T of
+// O^T += V^T P^T.  V^T is read from row-major tiles in LDS with ds_read_b64_tr_b16.
+//
+// Two kernels.  Few rows (up to 32: single tokens, drafted tokens) are bound by HBM: every wave streams tiles of its own
+// through a private ring in LDS and never meets the others until the end.  Many rows are bound by the matrix core: four
+// waves of 32 rows share tiles of 64 keys.
+//
+// Sharing out.  Lengths are on the device, so the launch is, too: all workgroups add up the cost of all units (request, key
+// head, tile of rows; cost = tiles of keys + a constant), and workgroup w takes the w-th of equal spans of that line.  A
+// unit that a span's end cuts leaves partial sums in the workspace; a second kernel puts them together.
+#include <algorithm>
+#include <cmath>
+
+#include "df_paged.h"
+
+namespace df {
+
+typedef unsigned short u16;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef u16 u16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef const __attribute__((address_space(4))) int const_int;
+
+struct Bf16 {
+  static constexpr u16 kExponent = 0x7f80;
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ unsigned pack(float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), bf16x2));
+  }
+};
+struct Fp16 {
+  static constexpr u16 kExponent = 0x7c00;
+  static __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ unsigned pack(float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{a, b}), f16x2));
+  }
+};
+
+struct PagedParams {
+  const char *q, *k_cur, *v_cur, *k_pages, *v_pages;
+  char *out;
+  float *lse;
+  const_int *table, *len, *cu, *sink, *win;        // read only: where the index is uniform, with scalar loads
+  int64_t q_tok, q_head, kc_head, o_tok, o_head;   // bytes
+  int64_t cap_stride;
+  unsigned kc_tok;           // bytes
+  int B, Hkv, Hq, G;
+  int page_log2, n_pages, max_pages;
+  int total, max_new, block;
+  int row_tiles;             // tiles of rows of max_new tokens
+  int units;                 // B * Hkv * row_tiles
+  float c;                   // scale * log2(e)
+  float slack;               // the reference follows a maximum that is more than this above it (8 bits)
+  float ln_unit;             // natural logarithm of one unit of c * score
+  char *ws;
+  int whole;                 // 1: no unit is ever cut, there is no second kernel
+};
+
+constexpr int kThreads = 256;
+constexpr int kUnitCost = 4;           // cost of a unit besides its tiles, in tiles
+constexpr int kSnap = 3;               // no piece of a cut unit has fewer tiles ...
+constexpr int kMinSpan = 8;            // ... than fit into the shortest span; units of up to kMinSpan tiles are not cut
+static_assert(2 * kSnap < kMinSpan, "a span inside a unit is a piece");
+
+// A request as one key head sees it.
+struct Request {
+  int n, q0;                 // new tokens and the first one's row
+  int L, s, w, held;         // tokens in the cache, sink, window, filled slots
+  bool bad;                  // more slots than the table has entries for
+};
+
+__device__ __forceinline__ Request request_of(const PagedParams &p, int b, int h) {
+  Request r;
+  const int c0 = clamp_int(p.cu[b], 0, p.total), c1 = clamp_int(p.cu[b + 1], c0, p.total);
+  const int64_t cap = b * p.cap_stride + h;
+  r.q0 = c0;
+  r.n = min(c1 - c0, p.max_new);
+  r.L = clamp_int(p.len[b], 0, kMaxLen);
+  r.s = clamp_int(p.sink[cap], 0, kMaxLen);
+  r.w = clamp_int(p.win[cap], 0, kMaxLen);
+  r.held = filled_slots(r.L, r.s, r.w);
+  const int64_t room = int64_t(p.max_pages) << p.page_log2;
+  r.bad = r.held > room;
+  if (r.bad) r.held = int(room);
+  return r;
+}
+
+// Slots that a causal block beginning at new token `first` sees: [0, a1) and [b0, b1).  Behind the sink they are a ring; what the
+// block does not see of it are the `first` oldest tokens (or, before the ring is full, those older than the window).
+struct Visible { int a1, b0, b1; };
+__device__ __forceinline__ Visible visible_slots(const Request &r, int first) {
+  Visible v;
+  const int sink = min(r.held, r.s), turn = r.L - r.s;
+  if (first >= r.w || turn <= 0) {
+    v.a1 = v.b0 = v.b1 = sink;
+  } else if (turn <= r.w) {
+    const int lo = r.L + first - r.w;
+    v.a1 = lo <= r.s ? r.held : sink;
+    v.b0 = lo <= r.s ? r.held : min(lo, r.held);
+    v.b1 = r.held;
+  } else if (first == 0) {
+    v.a1 = v.b0 = v.b1 = r.held;
+  } else {
+    const int at = turn % r.w;
+    const bool wraps = at > r.w - first;
+    v.a1 = min(r.held, wraps ? r.s : r.s + at);
+    v.b0 = min(r.held, wraps ? r.s + (at - (r.w - first)) : r.s + at + first);
+    v.b1 = min(r.held, wraps ? r.s + at : r.s + r.w);
+  }
+  return v;
+}
+
+// The key tiles of one unit: slots first, new tokens behind them, each in up to two runs of tiles.
+template <int KT>
+struct Tiles {
+  int nA, nB, nC, nD;        // tiles of the four runs
+  int firstB, firstD;        // first tile of the second runs (the first ones begin at 0)
+  __device__ __forceinline__ int count() const { return nA + nB + nC + nD; }
+  // Tile i: its first key, and whether that is a new token.
+  __device__ __forceinline__ int at(int i, bool &is_new) const {
+    is_new = i >= nA + nB;
+    if (is_new) {
+      i -= nA + nB;
+      return (i < nC ? i : firstD + i - nC) * KT;
+    }
+    return (i < nA ? i : firstB + i - nA) * KT;
+  }
+};
+
+struct RowRange {
+  int first0, first1;        // first tokens of the first and the last row's causal blocks
+  int end0, end1;            // and their ends
+};
+__device__ __forceinline__ RowRange row_range(const PagedParams &p, const Request &r, int row0, int rows) {
+  RowRange x;
+  const int block = min(p.block, max(r.n, 1));
+  const int i0 = row0 / p.G, i1 = min(r.n - 1, (row0 + rows - 1) / p.G);
+  x.first0 = i0 / block * block;
+  x.first1 = i1 / block * block;
+  x.end0 = min(x.first0 + block, r.n);
+  x.end1 = min(x.first1 + block, r.n);
+  return x;
+}
+
+template <int KT>
+__device__ __forceinline__ Tiles<KT> tiles_of(const PagedParams &p, const Request &r, const RowRange &x) {
+  Tiles<KT> t;
+  const Visible v = visible_slots(r, x.first0);
+  t.nA = (v.a1 + KT - 1) / KT;
+  t.firstB = max(v.b0 / KT, t.nA);
+  t.nB = v.b1 > v.b0 ? max(0, (v.b1 + KT - 1) / KT - t.firstB) : 0;
+  t.nC = t.nD = t.firstD = 0;
+  if (p.k_cur) {
+    const int c1 = clamp_int(r.s - r.L, 0, x.end1), d0 = max(0, x.first0 - r.w);
+    t.nC = (c1 + KT - 1) / KT;
+    t.firstD = max(d0 / KT, t.nC);
+    t.nD = max(0, (x.end1 + KT - 1) / KT - t.firstD);
+  }
+  return t;
+}
+
+// Unit u of the line: requests outermost, then key heads, then tiles of rows (neighbours read the same keys).
+struct Unit { int b, h, row0; };
+__device__ __forceinline__ Unit unit_of(const PagedParams &p, int u, int rows) {
+  const int e = u / p.row_tiles;
+  return Unit{e / p.Hkv, e % p.Hkv, (u - e * p.row_tiles) * rows};
+}
+
+// Cost of a unit on the line, 0 if it has no rows.
+template <int KT, int ROWS>
+__device__ __forceinline__ int unit_cost(const PagedParams &p, const Request &r, int row0) {
+  if (row0 >= r.n * p.G) return 0;
+  return kUnitCost + tiles_of<KT>(p, r, row_range(p, r, row0, ROWS)).count();
+}
+
+// Tile at which position x of a unit's part of the line (its first kUnitCost positions are no tiles) cuts its T tiles.
+__device__ __forceinline__ int cut_at(int64_t x, int T) {
+  if (T <= kMinSpan) return x <= 0 ? 0 : T;
+  const int64_t t = x - kUnitCost;
+  return t < kSnap ? 0 : t > T - kSnap ? T : int(t);
+}
+
+struct Span {
+  int index;                 // number of the span
+  int64_t begin, end;        // on the line
+  int unit;                  // the unit that `begin` lies in, -1: there is no span for this workgroup
+  int64_t unit_at;           // where that unit begins
+};
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return int64_t(unsigned(__builtin_amdgcn_readfirstlane(int(x)))) | int64_t(__builtin_amdgcn_readfirstlane(int(x >> 32))) << 32;
+}
+
+// This workgroup's span.  Every workgroup adds up all units; `scratch` is LDS, at least (kThreads / 64 + 2) 8-byte words.
+template <int KT, int ROWS>
+__device__ __forceinline__ Span my_span(const PagedParams &p, int64_t *scratch) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (p.units + kThreads - 1) / kThreads;
+  const int u0 = min(tid * per, p.units), u1 = min(u0 + per, p.units);
+  auto walk = [&](auto &&each) {
+    int known = -1;
+    Request r{};
+    for (int u = u0; u < u1; ++u) {
+      const int e = u / p.row_tiles;
+      if (e != known) {
+        known = e;
+        r = request_of(p, e / p.Hkv, e % p.Hkv);
+      }
+      each(u, unit_cost<KT, ROWS>(p, r, (u - e * p.row_tiles) * ROWS));
+    }
+  };
+  int64_t mine = 0;
+  walk([&](int, int cost) { mine += cost; });
+  int64_t incl = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(incl, d);
+    if (lane >= d) incl += y;
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  int64_t base = incl - mine, all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    const int64_t s = scratch[w];
+    if (w < wave) base += s;
+    all += s;
+  }
+  const int wgs = gridDim.x;
+  const int count = int(max(min(int64_t(wgs), all / kMinSpan), int64_t(all > 0)));
+  Span sp;
+  // Workgroups are dealt to the eight XCDs in turn: with a full launch an XCD takes neighbouring spans, which read the same keys.
+  sp.index = count == wgs && wgs % 8 == 0 ? int(blockIdx.x % 8) * (wgs / 8) + int(blockIdx.x / 8) : int(blockIdx.x);
+  sp.begin = sp.end = sp.unit_at = 0;
+  sp.unit = -1;
+  if (sp.index >= count) return sp;
+  sp.begin = uniform(all * sp.index / count);
+  sp.end = uniform(all * (sp.index + 1) / count);
+  if (mine > 0 && sp.begin >= base && sp.begin < base + mine) {
+    int64_t at = base;
+    walk([&](int u, int cost) {
+      if (sp.begin >= at && sp.begin < at + cost) {
+        scratch[kThreads / 64] = u;
+        scratch[kThreads / 64 + 1] = at;
+      }
+      at += cost;
+    });
+  }
+  __syncthreads();
+  sp.unit = int(uniform(scratch[kThreads / 64]));
+  sp.unit_at = uniform(scratch[kThreads / 64 + 1]);
+  return sp;
+}
+
+// Workspace: per span a note of its pieces of cut units, and behind the notes two slots of partial sums each.
+struct Note {
+  int tail_unit;             // the unit that the span begins and does not end, or -1 (its sums: slot 1)
+  int head;                  // piece of a unit that an earlier span begins: 0 none, 1 not its last, 2 its last (slot 0)
+};
+constexpr int kMaxSpans = 1024;
+constexpr size_t kNotesBytes = kMaxSpans * sizeof(Note);
+
+template <int ROWS, int D>
+struct PartialSlot {
+  static constexpr size_t kFloats = size_t(ROWS) * (D + 2);      // rows of O, then m, then l
+  __device__ static float *of(char *ws, int span, int which) {
+    return reinterpret_cast<float *>(ws + kNotesBytes) + (size_t(span) * 2 + which) * kFloats;
+  }
+};
+
+// ---- tiles in LDS ------------------------------------------------------------------------------------------------------------
+// A row's 16-byte chunks are stored at places that depend on the row, so that the reads of the operands meet no bank twice: the
+// hardware takes the lanes of a ds_read_b128 in groups of 16, {0-3, 12-15, 20-27} and so on, and 256 bytes a cycle.  K: chunk c
+// of the row that operand row m reads is at place c ^ m (D = 128, a row is all banks) or c ^ (m >> 1) (D = 64, two rows are).  V:
+// the 32 bytes of 16 output columns stay together, and move by the row's place among the eight that one pass reads.
+template <int D>
+struct Layout {
+  static constexpr int ROWB = 2 * D;
+  static constexpr int CH = D / 8;                       // chunks of a row
+  static constexpr int RPL = 1024 / ROWB;                // rows that one wave's load brings
+  static constexpr int LPG = 16 / RPL;                   // loads per group of 16 rows
+  __device__ static int k_turn(int row) {
+    const int m = (row & 3) | ((row >> 3) & 3) << 2;
+    return D == 128 ? m : m >> 1;
+  }
+  __device__ static int v_turn(int row) {
+    const int x = D == 128 ? (row & 3) | ((row >> 3) & 1) << 2 : ((row >> 1) & 1) | ((row >> 3) & 1) << 1;
+    return 2 * x;
+  }
+};
+// Key (of 32) that operand row m of block u (of two) holds; the block's scores 4 g + v, u = 0, 1 are then keys 8 g + 4 u + v.
+__device__ __forceinline__ int key_of_operand_row(int m, int u) { return 8 * (m >> 2) + 4 * u + (m & 3); }
+
+__device__ __forceinline__ unsigned lds_address(const void *ptr) { return unsigned(reinterpret_cast<uintptr_t>(ptr)); }
+
+__device__ __forceinline__ unsigned scalar(unsigned x) { return unsigned(__builtin_amdgcn_readfirstlane(int(x))); }
+
+// Where a group of 16 rows comes from (uniform).
+struct RowSource {
+  const char *k, *v;         // first row
+  unsigned stride, bytes;    // bytes between rows, addressable bytes (0: none; loads past them write zeros)
+};
+
+// 16 rows of K and V into LDS, asynchronously: LPG loads each.  `at` is the LDS address of the K rows, the V rows lie `v_off` behind them.
+// The statement is not one of the compiler's loads, so the reads of older tiles do not wait for it; whoever reads the rows waits for
+// them by count.  It begins with the wait states that a descriptor written by v_readlane needs, and keeps one instruction
+// between a write of m0 and the load that uses it.
+template <int D>
+__device__ __forceinline__ void load_group(const RowSource &src, const unsigned (&koff)[Layout<D>::LPG], const unsigned (&voff)[Layout<D>::LPG],
+                                           unsigned at, unsigned v_at) {
+  const uint64_t ka = reinterpret_cast<uint64_t>(src.k), va = reinterpret_cast<uint64_t>(src.v);
+  const unsigned bytes = scalar(src.bytes);
+  const u32x4 dk = {scalar(unsigned(ka)), scalar(unsigned(ka >> 32) & 0xffffu), bytes, 0x00020000u};
+  const u32x4 dv = {scalar(unsigned(va)), scalar(unsigned(va >> 32) & 0xffffu), bytes, 0x00020000u};
+  at = scalar(at);
+  v_at = scalar(v_at);
+  if constexpr (D == 128) {
+    asm volatile(
+        "s_nop 4\n\t"
+        "s_mov_b32 m0, %[at]\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k0], %[dk], 0 offen lds\n\t"
+        "s_add_u32 m0, %[at], 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k1], %[dk], 0 offen lds\n\t"
+        "s_add_u32 m0, %[at], 0x800\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k2], %[dk], 0 offen lds\n\t"
+        "s_add_u32 m0, %[at], 0xc00\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k3], %[dk], 0 offen lds\n\t"
+        "s_mov_b32 m0, %[vt]\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v0], %[dv], 0 offen lds\n\t"
+        "s_add_u32 m0, %[vt], 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v1], %[dv], 0 offen lds\n\t"
+        "s_add_u32 m0, %[vt], 0x800\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v2], %[dv], 0 offen lds\n\t"
+        "s_add_u32 m0, %[vt], 0xc00\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v3], %[dv], 0 offen lds"
+        ::[at] "s"(at), [vt] "s"(v_at), [dk] "s"(dk), [dv] "s"(dv), [k0] "v"(koff[0]), [k1] "v"(koff[1]), [k2] "v"(koff[2]),
+        [k3] "v"(koff[3]), [v0] "v"(voff[0]), [v1] "v"(voff[1]), [v2] "v"(voff[2]), [v3] "v"(voff[3])
+        : "memory", "scc");
+  } else {
+    asm volatile(
+        "s_nop 4\n\t"
+        "s_mov_b32 m0, %[at]\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k0], %[dk], 0 offen lds\n\t"
+        "s_add_u32 m0, %[at], 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %[k1], %[dk], 0 offen lds\n\t"
+        "s_mov_b32 m0, %[vt]\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v0], %[dv], 0 offen lds\n\t"
+        "s_add_u32 m0, %[vt], 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %[v1], %[dv], 0 offen lds"
+        ::[at] "s"(at), [vt] "s"(v_at), [dk] "s"(dk), [dv] "s"(dv), [k0] "v"(koff[0]), [k1] "v"(koff[1]), [v0] "v"(voff[0]), [v1] "v"(voff[1])
+        : "memory", "scc");
+  }
+}
+
+// What a wave needs to find rows: the request, and the lane's place in a load.
+template <int D>
+struct Loader {
+  const PagedParams &p;
+  const Request &r;
+  int h;
+  const_int *pages;          // the head's row of the block table
+  const char *k_cur, *v_cur; // the head's new tokens, first row of the request
+  int lane_row;              // row of a load's rows that the lane fetches
+  int lane_chunk;            // place of its chunk in the row
+  bool bad;                  // a page was no page of the pool
+
+  __device__ __forceinline__ Loader(const PagedParams &p_, const Request &r_, int b, int h_)
+      : p(p_), r(r_), h(h_), lane_row((threadIdx.x & 63) / Layout<D>::CH), lane_chunk((threadIdx.x & 63) % Layout<D>::CH), bad(r_.bad) {
+    pages = p.table + (int64_t(b) * p.Hkv + h) * p.max_pages;
+    k_cur = p.k_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
+    v_cur = p.v_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
+  }
+  // The 16 rows from key k0 on (a multiple of 16).
+  __device__ __forceinline__ RowSource source(int k0, bool is_new) {
+    RowSource s;
+    const int rows = clamp_int((is_new ? r.n : r.held) - k0, 0, 16);
+    if (is_new) {
+      s.k = k_cur + int64_t(k0) * p.kc_tok;
+      s.v = v_cur + int64_t(k0) * p.kc_tok;
+      s.stride = p.kc_tok;
+    } else {
+      int page = 0;
+      if (rows > 0) page = pages[k0 >> p.page_log2];
+      const bool no_page = unsigned(page) >= unsigned(p.n_pages);
+      bad |= no_page;
+      if (no_page) page = 0;
+      const int64_t at = ((int64_t(page) << p.page_log2) + (k0 & ((1 << p.page_log2) - 1))) * Layout<D>::ROWB;
+      s.k = p.k_pages + at;
+      s.v = p.v_pages + at;
+      s.stride = Layout<D>::ROWB;
+    }
+    s.bytes = rows > 0 ? unsigned(rows - 1) * s.stride + Layout<D>::ROWB : 0;
+    return s;
+  }
+  // Group `grp` of a tile (16 rows, place in the tile decides the swizzle) of keys from k0 on.
+  __device__ __forceinline__ void load(int k0, bool is_new, int grp, unsigned at, unsigned v_at) {
+    using L = Layout<D>;
+    const RowSource s = source(k0, is_new);
+    unsigned ko[L::LPG], vo[L::LPG];
+#pragma unroll
+    for (int i = 0; i < L::LPG; ++i) {
+      const int row = i * L::RPL + lane_row, place = grp * 16 + row;
+      const unsigned first = unsigned(row) * s.stride;
+      ko[i] = first + 16u * unsigned(lane_chunk ^ L::k_turn(place));
+      vo[i] = first + 16u * unsigned(lane_chunk ^ L::v_turn(place));
+    }
+    load_group<D>(s, ko, vo, at, v_at);
+  }
+};
+
+// ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
+
+// The lane's row in each of its blocks of 16 rows, as masks need it.
+struct RowMask {
+  int lim_hist, lim_new;     // lowest position (window) that the row sees of the cache and of the new tokens
+  int end;                   // new tokens before this one
+};
+
+template <class T, int D, int KB, int QB>      // KB blocks of 16 keys, QB blocks of 16 rows
+struct Rows {
+  static constexpr int KS = D / 32, DB = D / 16;
+  s16x8 q[KS][QB];
+  f32x4 o[DB][QB];
+  float m[QB], l[QB];
+  RowMask mask[QB];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      m[qb] = -INFINITY;
+      l[qb] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // The lane's share of rows row0 + 16 qb + lane % 16; rows behind the request's last repeat it and are not stored.
+  __device__ __forceinline__ void load_q(const PagedParams &p, const Request &r, int h, int row0) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, block = min(p.block, max(r.n, 1));
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int row = min(row0 + 16 * qb + (lane & 15), r.n * p.G - 1);
+      const int i = row / p.G, head = h * p.G + row - i * p.G;
+      const char *src = p.q + int64_t(r.q0 + i) * p.q_tok + head * p.q_head + 16 * g;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q[ks][qb] = *reinterpret_cast<const s16x8 *>(src + 64 * ks);
+      const int first = i / block * block;
+      mask[qb].end = min(first + block, r.n);
+      mask[qb].lim_new = first - r.w;
+      mask[qb].lim_hist = r.L + first - r.w;
+    }
+  }
+
+  // S^T: scores of keys 32 (kb / 2) + 8 g + 4 (kb % 2) + v of the lane's quarter g.
+  __device__ __forceinline__ void scores(const char *k, f32x4 (&s)[KB][QB]) const {
+    const int lane = threadIdx.x & 63, g = lane >> 4, mrow = lane & 15;
+    using L = Layout<D>;
+    const char *base = k + key_of_operand_row(mrow, 0) * L::ROWB;
+    const int turn = L::k_turn(key_of_operand_row(mrow, 0));
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const char *at = base + 16 * ((4 * ks + g) ^ turn);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const s16x8 a = *reinterpret_cast<const s16x8 *>(at + (32 * (kb >> 1) + 4 * (kb & 1)) * L::ROWB);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+          s[kb][qb] = T::mfma(a, q[ks][qb], ks ? s[kb][qb] : f32x4{0.f, 0.f, 0.f, 0.f});
+      }
+    }
+  }
+
+  // Scores of keys that a row does not see become minus infinity.
+  __device__ __forceinline__ void hide(const Request &r, int k0, bool is_new, f32x4 (&s)[KB][QB]) const {
+    const int g = (threadIdx.x & 63) >> 4;
+    const int turn = max(r.L - r.s, 0);
+    const bool wrapped = turn > r.w;
+    const int at = wrapped && r.w > 0 ? turn % r.w : 0;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v;
+        int pos = key;                                   // position, or the largest where the window does not matter
+        if (is_new) {
+          if (key < r.s - r.L) pos = INT32_MAX;
+        } else if (key < r.s) {
+          pos = INT32_MAX;
+        } else if (wrapped) {
+          const int k = key - r.s;
+          pos = r.L - at + k - (k < at ? 0 : r.w);
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const bool seen = is_new ? key < mask[qb].end && pos >= mask[qb].lim_new : key < r.held && pos >= mask[qb].lim_hist;
+          s[kb][qb][v] = seen ? s[kb][qb][v] : -INFINITY;
+        }
+      }
+  }
+
+  // Weights of a tile, packed as the second product's operand; the reference moves up where a score is `slack` above it, so
+  // weights stay below 2^8 and moves are rare.
+  __device__ __forceinline__ void weights(const PagedParams &p, f32x4 (&s)[KB][QB], s16x8 (&w)[KB / 2][QB]) {
+    float top[QB];
+    bool up = false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      top[qb] = s[0][qb][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top[qb] = fmaxf(top[qb], s[kb][qb][v]);
+      up |= top[qb] > m[qb] + p.slack;                   // m = -inf: any score that is not
+    }
+    if (__builtin_amdgcn_ballot_w64(up)) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        float t = top[qb];
+        t = fmaxf(t, __shfl_xor(t, 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        t = fmaxf(t, m[qb]);
+        // no key with a score yet: the reference stays, and nothing is scaled by the NaN of inf - inf
+        const float scale = t == m[qb] ? 1.f : __builtin_amdgcn_exp2f((m[qb] - t) * p.c);
+        m[qb] = t;
+        l[qb] *= scale;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db][qb] *= scale;
+      }
+    }
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const float mc = m[qb] == -INFINITY ? 0.f : m[qb] * p.c;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[kb][qb][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][qb][v], p.c, -mc));
+      f32x4 sum = s[0][qb];
+#pragma unroll
+      for (int kb = 1; kb < KB; ++kb) sum += s[kb][qb];
+      l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int ts = 0; ts < KB / 2; ++ts) {
+        u32x4 x;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) x[2 * u + v] = T::pack(s[2 * ts + u][qb][2 * v], s[2 * ts + u][qb][2 * v + 1]);
+        w[ts][qb] = __builtin_bit_cast(s16x8, x);
+      }
+    }
+  }
+
+  __device__ __forceinline__ static s16x8 v_operand(const char *base, int turn, int ts, int db) {
+    using L = Layout<D>;
+    const char *at = base + 32 * (db ^ turn) + 32 * ts * L::ROWB;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * L::ROWB));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+
+  // O^T += V^T P^T.
+  __device__ __forceinline__ void values(const char *v, const s16x8 (&w)[KB / 2][QB]) {
+    using L = Layout<D>;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+    const int row = 8 * g + (j >> 2), turn = L::v_turn(row) / 2;
+    const char *base = v + row * L::ROWB + 8 * (j & 3);
+#pragma unroll
+    for (int ts = 0; ts < KB / 2; ++ts)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const s16x8 a = v_operand(base, turn, ts, db);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) o[db][qb] = T::mfma(a, w[ts][qb], o[db][qb]);
+      }
+  }
+
+  // The same for a tile that some rows do not see all of.  A weight of zero does not hide an infinity or a NaN from the product, so
+  // those take part as what they do to a row that sees them: three products of their indicators say which rows do.
+  __device__ __forceinline__ void values_hidden(const char *v, const s16x8 (&w)[KB / 2][QB]) {
+    using L = Layout<D>;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+    const int row = 8 * g + (j >> 2), turn = L::v_turn(row) / 2;
+    const char *base = v + row * L::ROWB + 8 * (j & 3);
+    bool odd = false;
+#pragma unroll
+    for (int ts = 0; ts < KB / 2; ++ts)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const s16x8 a = v_operand(base, turn, ts, db);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) odd |= (u16(a[k]) & T::kExponent) == T::kExponent;
+      }
+    if (!__builtin_amdgcn_ballot_w64(odd)) return values(v, w);
+    const unsigned one_bits = T::pack(1.f, 1.f);
+    const short one = short(one_bits);
+#pragma unroll 1
+    for (int ts = 0; ts < KB / 2; ++ts)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const s16x8 a = v_operand(base, turn, ts, db);
+        s16x8 fin, pos, neg, nan;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const u16 x = u16(a[k]);
+          const bool f = (x & T::kExponent) != T::kExponent;
+          fin[k] = f ? a[k] : short(0);
+          pos[k] = x == T::kExponent ? one : short(0);
+          neg[k] = x == (T::kExponent | 0x8000u) ? one : short(0);
+          nan[k] = !f && (x & 0x7fffu) != T::kExponent ? one : short(0);
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+          const s16x8 b = ts == 0 ? w[0][qb] : w[KB / 2 - 1][qb];
+          const f32x4 up = T::mfma(pos, b, zero), down = T::mfma(neg, b, zero), none = T::mfma(nan, b, zero);
+          f32x4 x = T::mfma(fin, b, o[db][qb]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (up[i] != 0.f) x[i] += INFINITY;
+            if (down[i] != 0.f) x[i] -= INFINITY;
+            if (none[i] != 0.f) x[i] = NAN;
+          }
+          o[db][qb] = x;
+        }
+      }
+  }
+};
+
+// Whether every row of the range sees all KT keys from k0 on.
+template <int KT>
+__device__ __forceinline__ bool all_seen(const Request &r, const RowRange &x, const Visible &v, int k0, bool is_new) {
+  if (!is_new) return k0 + KT <= v.a1 || (k0 >= v.b0 && k0 + KT <= v.b1);
+  const int c1 = clamp_int(r.s - r.L, 0, x.end0);
+  return k0 + KT <= c1 || (k0 >= x.first1 - r.w && k0 + KT <= x.end0);
+}
+
+template <class T>
+__device__ __forceinline__ void store_row4(const PagedParams &p, const Request &r, int h, int row, int col, f32x4 x) {
+  const int i = row / p.G, head = h * p.G + row - i * p.G;
+  char *dst = p.out + int64_t(r.q0 + i) * p.o_tok + head * p.o_head + 2 * col;
+  uint2 y;
+  y.x = T::pack(x[0], x[1]);
+  y.y = T::pack(x[2], x[3]);
+  *reinterpret_cast<uint2 *>(dst) = y;
+}
+// m and l of a finished row: l = 0 where the row sees nothing.
+__device__ __forceinline__ void store_lse(const PagedParams &p, const Request &r, int h, int row, float m, float l) {
+  const int i = row / p.G, head = h * p.G + row - i * p.G;
+  const float log2_sum = m * p.c + __builtin_amdgcn_logf(l);
+  p.lse[int64_t(head) * p.total + r.q0 + i] = l == 0.f ? -INFINITY : log2_sum * p.ln_unit;
+}
+
+// ---- many rows: four waves of 32 share tiles of 64 keys ---------------------------------------------------------------------------
+
+constexpr int kManyRows = 128, kManyKeys = 64;
+
+template <class T, int D>
+__global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedParams p) {
+  using L = Layout<D>;
+  constexpr int KT = kManyKeys, ROWS = kManyRows, TILE = KT * L::ROWB;
+  __shared__ __attribute__((aligned(1024))) char tiles[4 * TILE];      // two buffers of K and V
+  __shared__ int64_t scratch[kThreads / 64 + 2];
+  __shared__ int poison;                 // the last unit of which a page was none
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (tid == 0) poison = -1;
+  const Span sp = my_span<KT, ROWS>(p, scratch);
+  Note note{-1, 0};
+  const unsigned lds0 = lds_address(tiles);
+  int64_t at = sp.unit_at;
+  for (int u = max(sp.unit, 0); u < p.units && at < sp.end; ++u) {
+    const Unit un = unit_of(p, u, ROWS);
+    const Request r = request_of(p, un.b, un.h);
+    if (un.row0 >= r.n * p.G) continue;
+    const RowRange x = row_range(p, r, un.row0, ROWS);
+    const Tiles<KT> tl = tiles_of<KT>(p, r, x);
+    const int nt = tl.count();
+    const int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
+    const bool owns = sp.begin <= at;
+    at += kUnitCost + nt;
+    if (t0 >= t1 && !(nt == 0 && owns)) continue;
+
+    Rows<T, D, KT / 16, 2> rows;
+    rows.clear();
+    Loader<D> ld(p, r, un.b, un.h);
+    const Visible inner = visible_slots(r, x.first1);
+    const int row0 = un.row0 + 32 * wave;
+    if (t0 < t1) {
+      bool is_new;
+      int k0 = tl.at(t0, is_new);
+      ld.load(k0 + 16 * wave, is_new, wave, lds0 + wave * 16 * L::ROWB, lds0 + TILE + wave * 16 * L::ROWB);
+      rows.load_q(p, r, un.h, row0);
+      for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        // the wave's rows of this tile have landed, and every wave is done with the tile before
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        bool next_new = false;
+        int next_k0 = 0;
+        if (t + 1 < t1) {
+          next_k0 = tl.at(t + 1, next_new);
+          const unsigned to = lds0 + (buf ^ 1) * 2 * TILE + wave * 16 * L::ROWB;
+          ld.load(next_k0 + 16 * wave, next_new, wave, to, to + TILE);
+        }
+        if (row0 < r.n * p.G) {
+          const char *k = tiles + buf * 2 * TILE, *v = k + TILE;
+          f32x4 s[KT / 16][2];
+          s16x8 w[KT / 32][2];
+          rows.scores(k, s);
+          const bool hidden = !all_seen<KT>(r, x, inner, k0, is_new);
+          if (hidden) rows.hide(r, k0, is_new, s);
+          rows.weights(p, s, w);
+          if (hidden) rows.values_hidden(v, w); else rows.values(v, w);
+        }
+        k0 = next_k0;
+        is_new = next_new;
+      }
+    }
+    if (ld.bad) poison = u;
+    __syncthreads();                     // all waves are done with the tiles and have said what pages they met
+    const bool nan = poison == u;
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+      float l = rows.l[qb];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (nan) l = NAN;
+      const int row = row0 + 16 * qb + (lane & 15), g = lane >> 4;
+      if (t0 == 0 && t1 == nt) {
+        if (row < r.n * p.G) {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+          for (int db = 0; db < L::CH / 2; ++db) store_row4<T>(p, r, un.h, row, 16 * db + 4 * g, rows.o[db][qb] * inv);
+          if (p.lse && g == 0) store_lse(p, r, un.h, row, rows.m[qb], l);
+        }
+      } else {
+        float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, t0 == 0);
+        const int in_unit = row - un.row0;
+#pragma unroll
+        for (int db = 0; db < L::CH / 2; ++db) *reinterpret_cast<f32x4 *>(slot + in_unit * D + 16 * db + 4 * g) = rows.o[db][qb];
+        if (g == 0) {
+          slot[ROWS * D + in_unit] = rows.m[qb];
+          slot[ROWS * (D + 1) + in_unit] = l;
+        }
+      }
+    }
+    if (t0 == 0 && t1 < nt) note.tail_unit = u;
+    if (t0 > 0) note.head = t1 == nt ? 2 : 1;
+    __syncthreads();                     // the poison of this piece has been read, the tiles may be loaded again
+  }
+  if (!p.whole && tid == 0) reinterpret_cast<Note *>(p.ws)[sp.index] = note;
+}
+
+// ---- few rows: every wave streams tiles of its own ----------------------------------------------------------------------------------
+
+constexpr int kFewKeys = 32, kFewWaves = 4;
+
+template <class T, int D, int QB>
+__global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParams p) {
+  using L = Layout<D>;
+  constexpr int KT = kFewKeys, ROWS = 16 * QB, TILE = KT * L::ROWB, RING = 2;
+  constexpr int LOADS = 4 * L::LPG;                                    // loads of a tile, K and V
+  __shared__ __attribute__((aligned(1024))) char tiles[kFewWaves][RING][2][TILE];
+  __shared__ int64_t scratch[kThreads / 64 + 2];
+  __shared__ float stats[kFewWaves][2][ROWS];
+  __shared__ int poison;                 // the last unit of which a page was none
+  static_assert(sizeof(float) * ROWS * D <= sizeof(tiles[0]), "a wave's sums pass through its tiles");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (tid == 0) poison = -1;
+  const Span sp = my_span<KT, ROWS>(p, scratch);
+  Note note{-1, 0};
+  const unsigned lds0 = lds_address(&tiles[wave][0][0][0]);
+  int64_t at = sp.unit_at;
+  for (int u = max(sp.unit, 0); u < p.units && at < sp.end; ++u) {
+    const Unit un = unit_of(p, u, ROWS);
+    const Request r = request_of(p, un.b, un.h);
+    if (un.row0 >= r.n * p.G) continue;
+    const RowRange x = row_range(p, r, un.row0, ROWS);
+    const Tiles<KT> tl = tiles_of<KT>(p, r, x);
+    const int nt = tl.count();
+    const int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
+    const bool owns = sp.begin <= at;
+    at += kUnitCost + nt;
+    if (t0 >= t1 && !(nt == 0 && owns)) continue;
+
+    Rows<T, D, 2, QB> rows;
+    rows.clear();
+    Loader<D> ld(p, r, un.b, un.h);
+    const Visible inner = visible_slots(r, x.first1);
+    auto issue = [&](int t, int buf) {
+      bool is_new;
+      const int k0 = tl.at(t, is_new);
+      const unsigned to = lds0 + buf * 2 * TILE;
+#pragma unroll
+      for (int grp = 0; grp < 2; ++grp)
+        ld.load(k0 + 16 * grp, is_new, grp, to + grp * 16 * L::ROWB, to + TILE + grp * 16 * L::ROWB);
+    };
+    int t = t0 + wave;
+    if (t < t1) issue(t, 0);
+    if (t + kFewWaves < t1) issue(t + kFewWaves, 1);
+    rows.load_q(p, r, un.h, un.row0);
+    for (int buf = 0; t < t1; t += kFewWaves, buf ^= 1) {
+      // this tile has landed, the next one may still be on its way
+      if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      bool is_new;
+      const int k0 = tl.at(t, is_new);
+      const char *k = &tiles[wave][buf][0][0], *v = &tiles[wave][buf][1][0];
+      f32x4 s[2][QB];
+      s16x8 w[1][QB];
+      rows.scores(k, s);
+      const bool hidden = !all_seen<KT>(r, x, inner, k0, is_new);
+      if (hidden) rows.hide(r, k0, is_new, s);
+      rows.weights(p, s, w);
+      if (hidden) rows.values_hidden(v, w); else rows.values(v, w);
+      if (t + 2 * kFewWaves < t1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the reads of this buffer are done
+        issue(t + 2 * kFewWaves, buf);
+      }
+    }
+    if (ld.bad) poison = u;
+    // the four waves' sums meet in LDS: references, row sums, outputs
+    float *mine = reinterpret_cast<float *>(&tiles[wave][0][0][0]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float l = rows.l[qb];
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      const int row = 16 * qb + (lane & 15), g = lane >> 4;
+#pragma unroll
+      for (int db = 0; db < L::CH / 2; ++db) *reinterpret_cast<f32x4 *>(mine + row * D + 16 * db + 4 * g) = rows.o[db][qb];
+      if (g == 0) {
+        stats[wave][0][row] = rows.m[qb];
+        stats[wave][1][row] = l;
+      }
+    }
+    __syncthreads();
+    const bool nan = poison == u, whole = t0 == 0 && t1 == nt;
+    float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, t0 == 0);
+    for (int i = tid; i < ROWS * D / 4; i += kThreads) {
+      const int in_unit = i / (D / 4), col = 4 * (i % (D / 4)), row = un.row0 + in_unit;
+      if (row >= r.n * p.G) continue;
+      float m = stats[0][0][in_unit];
+#pragma unroll
+      for (int w = 1; w < kFewWaves; ++w) m = fmaxf(m, stats[w][0][in_unit]);
+      float l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        const float mw = stats[w][0][in_unit];
+        const float f = mw == m ? 1.f : __builtin_amdgcn_exp2f((mw - m) * p.c);
+        l += f * stats[w][1][in_unit];
+        o += f * *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(&tiles[w][0][0][0]) + in_unit * D + col);
+      }
+      if (nan) l = NAN;
+      if (whole) {
+        store_row4<T>(p, r, un.h, row, col, o * (l == 0.f ? 0.f : 1.f / l));
+        if (p.lse && col == 0) store_lse(p, r, un.h, row, m, l);
+      } else {
+        *reinterpret_cast<f32x4 *>(slot + in_unit * D + col) = o;
+        if (col == 0) {
+          slot[ROWS * D + in_unit] = m;
+          slot[ROWS * (D + 1) + in_unit] = l;
+        }
+      }
+    }
+    if (t0 == 0 && t1 < nt) note.tail_unit = u;
+    if (t0 > 0) note.head = t1 == nt ? 2 : 1;
+    __syncthreads();                     // the tiles may be loaded again
+  }
+  if (!p.whole && tid == 0) reinterpret_cast<Note *>(p.ws)[sp.index] = note;
+}
+
+// ---- cut units ------------------------------------------------------------------------------------------------------------------------
+
+// Workgroup (w, y): if span w begins a unit that it does not end, rows y * kMergeRows ... of it are put together from its slot 1 and slot 0
+// of the spans behind it, up to the one that holds the unit's end.
+constexpr int kMergeThreads = 256;
+
+template <class T, int D, int ROWS, int KT>
+__global__ __launch_bounds__(kMergeThreads) void df_paged_merge_kernel(const PagedParams p, int spans) {
+  constexpr int V = D / 4, RPB = kMergeThreads / V;      // four columns a thread, rows of a workgroup
+  const Note *notes = reinterpret_cast<const Note *>(p.ws);
+  const int w0 = blockIdx.x, u = notes[w0].tail_unit;
+  if (u < 0 || u >= p.units) return;
+  const Unit un = unit_of(p, u, ROWS);
+  const Request r = request_of(p, un.b, un.h);
+  const int in_unit = blockIdx.y * RPB + threadIdx.x / V, row = un.row0 + in_unit, col = 4 * (threadIdx.x % V);
+  if (row >= r.n * p.G) return;
+  const float *slot = PartialSlot<ROWS, D>::of(p.ws, w0, 1);
+  float m = slot[ROWS * D + in_unit], l = slot[ROWS * (D + 1) + in_unit];
+  f32x4 o = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
+  for (int w = w0 + 1; w < spans; ++w) {
+    const int head = notes[w].head;
+    slot = PartialSlot<ROWS, D>::of(p.ws, w, 0);
+    const float m1 = slot[ROWS * D + in_unit], l1 = slot[ROWS * (D + 1) + in_unit];
+    const f32x4 o1 = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
+    const float t = fmaxf(m, m1);
+    const float f0 = m == t ? 1.f : __builtin_amdgcn_exp2f((m - t) * p.c), f1 = m1 == t ? 1.f : __builtin_amdgcn_exp2f((m1 - t) * p.c);
+    m = t;
+    l = f0 * l + f1 * l1;
+    o = f0 * o + f1 * o1;
+    if (head != 1) break;
+  }
+  store_row4<T>(p, r, un.h, row, col, o * (l == 0.f ? 0.f : 1.f / l));
+  if (p.lse && col == 0) store_lse(p, r, un.h, row, m, l);
+}
+
+}  // namespace df
+
+using namespace df;
+
+// Which kernel: the rows that max_new tokens make of a key head's query heads decide.  Up to 32 rows the tile of rows is
+// one wave's, and streaming the keys bounds the call; beyond, four waves share them.
+namespace {
+struct Shape {
+  int rows, keys;            // of a tile
+  int spans;                 // most spans
+};
+const_int *as_const(const int32_t *x) { return (const_int *)(uintptr_t)x; }
+Shape shape_of(int64_t rows) {
+  if (rows <= 16) return {16, kFewKeys, 256};
+  if (rows <= 32) return {32, kFewKeys, 256};
+  return {kManyRows, kManyKeys, 512};
+}
+bool sizes_ok(int64_t H_q, int64_t H_kv, int64_t d, int64_t max_new) {
+  return H_kv > 0 && H_kv <= kMaxHeads && H_q > 0 && H_q % H_kv == 0 && H_q / H_kv <= 64 && (d == 64 || d == 128) && max_new > 0 &&
+         max_new * (H_q / H_kv) <= kMaxLen;
+}
+}  // namespace
+
+extern "C" size_t df_paged_workspace_bytes(int32_t H_q, int32_t H_kv, int32_t d, int32_t max_new) {
+  if (!sizes_ok(H_q, H_kv, d, max_new)) return 0;
+  const Shape s = shape_of(int64_t(max_new) * (H_q / H_kv));
+  return kNotesBytes + size_t(s.spans) * 2 * s.rows * (d + 2) * sizeof(float);
+}
+
+namespace {
+template <class T, int D>
+df_status launch_attn(const PagedParams &p, const Shape &s, hipStream_t stream) {
+  const dim3 threads(kThreads);
+  if (s.rows == 16)
+    hipLaunchKernelGGL((df_paged_few_kernel<T, D, 1>), dim3(s.spans), threads, 0, stream, p);
+  else if (s.rows == 32)
+    hipLaunchKernelGGL((df_paged_few_kernel<T, D, 2>), dim3(s.spans), threads, 0, stream, p);
+  else
+    hipLaunchKernelGGL((df_paged_many_kernel<T, D>), dim3(s.spans), threads, 0, stream, p);
+  if (df_status st = launch_status()) return st;
+  if (p.whole) return DF_OK;
+  const int per = kMergeThreads / (D / 4);
+  const int rows = int(std::min<int64_t>(s.rows, int64_t(p.max_new) * p.G));
+  const dim3 grid(s.spans, (rows + per - 1) / per);
+  if (s.rows == 16)
+    hipLaunchKernelGGL((df_paged_merge_kernel<T, D, 16, kFewKeys>), grid, dim3(kMergeThreads), 0, stream, p, s.spans);
+  else if (s.rows == 32)
+    hipLaunchKernelGGL((df_paged_merge_kernel<T, D, 32, kFewKeys>), grid, dim3(kMergeThreads), 0, stream, p, s.spans);
+  else
+    hipLaunchKernelGGL((df_paged_merge_kernel<T, D, kManyRows, kManyKeys>), grid, dim3(kMergeThreads), 0, stream, p, s.spans);
+  return launch_status();
+}
+}  // namespace
+
+extern "C" df_status df_paged_attn(const df_paged_attn_args *a, void *stream) {
+  if (!a) return DF_ERR_NULL;
+  if (df_status s = check_paged_cache(a->cache)) return s;
+  const df_paged_cache *c = a->cache;
+  if (!a->q || !a->out || !a->cu_new || !a->k_cur != !a->v_cur) return DF_ERR_NULL;
+  if (a->H_q <= 0 || a->total_new <= 0 || a->max_new <= 0 || a->block <= 0 || a->H_q % c->H_kv) return DF_ERR_SHAPE;
+  if (a->H_q / c->H_kv > 64) return DF_ERR_UNSUPPORTED;
+  if (a->max_new > a->total_new) return DF_ERR_SHAPE;
+  if (!(a->softmax_scale > 0.f) || !std::isfinite(a->softmax_scale)) return DF_ERR_RANGE;
+  if (a->total_new > kMaxLen || !sizes_ok(a->H_q, c->H_kv, c->d, a->max_new)) return DF_ERR_RANGE;
+  if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride_tok) || !stride_ok(a->o_stride_tok) ||
+      (a->H_q > 1 && (!stride_ok(a->q_stride_head) || !stride_ok(a->o_stride_head))))
+    return DF_ERR_ALIGN;
+  if (a->k_cur && (!aligned16(a->k_cur) || !aligned16(a->v_cur) || !stride_ok(a->kc_stride_tok) ||
+                   (c->H_kv > 1 && !stride_ok(a->kc_stride_head))))
+    return DF_ERR_ALIGN;
+  if (a->k_cur && a->kc_stride_tok > (1 << 26)) return DF_ERR_RANGE;       // 16 rows are addressed by 32 bits
+  const int G = a->H_q / c->H_kv;
+  const int64_t rows = int64_t(a->max_new) * G;
+  const Shape s = shape_of(rows);
+  const int64_t row_tiles = (rows + s.rows - 1) / s.rows, units = row_tiles * c->B * c->H_kv;
+  if (units > kMaxLen) return DF_ERR_RANGE;
+  if (!a->workspace || a->workspace_bytes < df_paged_workspace_bytes(a->H_q, c->H_kv, c->d, a->max_new)) return DF_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return DF_ERR_ALIGN;
+
+  PagedParams p{};
+  p.q = static_cast<const char *>(a->q);
+  p.k_cur = static_cast<const char *>(a->k_cur);
+  p.v_cur = static_cast<const char *>(a->v_cur);
+  p.k_pages = static_cast<const char *>(c->k_pages);
+  p.v_pages = static_cast<const char *>(c->v_pages);
+  p.out = static_cast<char *>(a->out);
+  p.lse = a->lse_out;
+  p.table = as_const(c->block_table); p.len = as_const(c->len); p.cu = as_const(a->cu_new);
+  p.sink = as_const(c->sink_cap); p.win = as_const(c->win_cap);
+  p.q_tok = 2 * a->q_stride_tok; p.q_head = 2 * a->q_stride_head;
+  p.o_tok = 2 * a->o_stride_tok; p.o_head = 2 * a->o_stride_head;
+  p.kc_tok = unsigned(2 * a->kc_stride_tok); p.kc_head = 2 * a->kc_stride_head;
+  p.cap_stride = c->cap_stride;
+  p.B = c->B; p.Hkv = c->H_kv; p.Hq = a->H_q; p.G = G;
+  p.page_log2 = log2_of(c->page_tokens); p.n_pages = c->n_pages; p.max_pages = c->max_pages;
+  p.total = a->total_new; p.max_new = a->max_new; p.block = a->block;
+  p.row_tiles = int(row_tiles);
+  p.units = int(units);
+  p.c = a->softmax_scale * 1.4426950408889634f;
+  p.ln_unit = float(double(a->softmax_scale) / double(p.c));
+  p.slack = 8.f / p.c;
+  p.ws = static_cast<char *>(a->workspace);
+  // the most tiles that a unit can have: its slots and its new tokens, each in two runs
+  const int64_t slots = int64_t(c->max_pages) * c->page_tokens;
+  const int64_t most = (slots + s.keys - 1) / s.keys + 1 + (a->k_cur ? (int64_t(a->max_new) + s.keys - 1) / s.keys + 1 : 0);
+  p.whole = most <= kMinSpan;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (c->dtype == DF_BF16) return c->d == 128 ? launch_attn<Bf16, 128>(p, s, st) : launch_attn<Bf16, 64>(p, s, st);
+  return c->d == 128 ? launch_attn<Fp16, 128>(p, s, st) : launch_attn<Fp16, 64>(p, s, st);
+}
