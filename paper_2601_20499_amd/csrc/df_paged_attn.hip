@@ -72,7 +72,6 @@ struct PagedParams {
   int row_tiles;             // tiles of rows of max_new tokens
   int units;                 // B * Hkv * row_tiles
   float c;                   // scale * log2(e)
-  float slack;               // the reference follows a maximum that is more than this above it (8 bits)
   float ln_unit;             // natural logarithm of one unit of c * score
   char *ws;
   int whole;                 // 1: no unit is ever cut, there is no second kernel
@@ -138,15 +137,6 @@ struct Tiles {
   int nA, nB, nC, nD;        // tiles of the four runs
   int firstB, firstD;        // first tile of the second runs (the first ones begin at 0)
   __device__ __forceinline__ int count() const { return nA + nB + nC + nD; }
-  // Tile i: its first key, and whether that is a new token.
-  __device__ __forceinline__ int at(int i, bool &is_new) const {
-    is_new = i >= nA + nB;
-    if (is_new) {
-      i -= nA + nB;
-      return (i < nC ? i : firstD + i - nC) * KT;
-    }
-    return (i < nA ? i : firstB + i - nA) * KT;
-  }
 };
 
 struct RowRange {
@@ -362,61 +352,112 @@ __device__ __forceinline__ void load_group(const RowSource &src, const unsigned 
   }
 }
 
-// What a wave needs to find rows: the request, and the lane's place in a load.
-template <int D>
-struct Loader {
+// Walks the tiles of a unit in the order of Tiles, `ahead` of the tile that is computed, and brings their rows.  Uniform but for
+// the lane's offsets.  The page of the next tile's rows is looked up one step before it is used.
+template <int D, int KT, int GROUPS>                     // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
+struct Cursor {
+  using L = Layout<D>;
   const PagedParams &p;
   const Request &r;
-  int h;
+  const Tiles<KT> &tl;
+  const int grp0;
   const_int *pages;          // the head's row of the block table
-  const char *k_cur, *v_cur; // the head's new tokens, first row of the request
+  const char *k_cur, *v_cur; // the head's new tokens, the request's first row
   int lane_row;              // row of a load's rows that the lane fetches
-  int lane_chunk;            // place of its chunk in the row
+  unsigned kc[GROUPS][L::LPG], vc[GROUPS][L::LPG];       // and its chunk's place in the source row, in bytes
+  int k0, end;               // first key of the tile, end of its run of tiles
+  bool is_new;
+  int page[GROUPS];
   bool bad;                  // a page was no page of the pool
 
-  __device__ __forceinline__ Loader(const PagedParams &p_, const Request &r_, int b, int h_)
-      : p(p_), r(r_), h(h_), lane_row((threadIdx.x & 63) / Layout<D>::CH), lane_chunk((threadIdx.x & 63) % Layout<D>::CH), bad(r_.bad) {
+  __device__ __forceinline__ Cursor(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, int b, int h, int grp0_, int t)
+      : p(p_), r(r_), tl(tl_), grp0(grp0_), lane_row((threadIdx.x & 63) / L::CH), bad(r_.bad) {
     pages = p.table + (int64_t(b) * p.Hkv + h) * p.max_pages;
     k_cur = p.k_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
     v_cur = p.v_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
-  }
-  // The 16 rows from key k0 on (a multiple of 16).
-  __device__ __forceinline__ RowSource source(int k0, bool is_new) {
-    RowSource s;
-    const int rows = clamp_int((is_new ? r.n : r.held) - k0, 0, 16);
-    if (is_new) {
-      s.k = k_cur + int64_t(k0) * p.kc_tok;
-      s.v = v_cur + int64_t(k0) * p.kc_tok;
-      s.stride = p.kc_tok;
-    } else {
-      int page = 0;
-      if (rows > 0) page = pages[k0 >> p.page_log2];
-      const bool no_page = unsigned(page) >= unsigned(p.n_pages);
-      bad |= no_page;
-      if (no_page) page = 0;
-      const int64_t at = ((int64_t(page) << p.page_log2) + (k0 & ((1 << p.page_log2) - 1))) * Layout<D>::ROWB;
-      s.k = p.k_pages + at;
-      s.v = p.v_pages + at;
-      s.stride = Layout<D>::ROWB;
-    }
-    s.bytes = rows > 0 ? unsigned(rows - 1) * s.stride + Layout<D>::ROWB : 0;
-    return s;
-  }
-  // Group `grp` of a tile (16 rows, place in the tile decides the swizzle) of keys from k0 on.
-  __device__ __forceinline__ void load(int k0, bool is_new, int grp, unsigned at, unsigned v_at) {
-    using L = Layout<D>;
-    const RowSource s = source(k0, is_new);
-    unsigned ko[L::LPG], vo[L::LPG];
+    const int lane_chunk = (threadIdx.x & 63) % L::CH;
 #pragma unroll
-    for (int i = 0; i < L::LPG; ++i) {
-      const int row = i * L::RPL + lane_row, place = grp * 16 + row;
-      const unsigned first = unsigned(row) * s.stride;
-      ko[i] = first + 16u * unsigned(lane_chunk ^ L::k_turn(place));
-      vo[i] = first + 16u * unsigned(lane_chunk ^ L::v_turn(place));
+    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+      for (int i = 0; i < L::LPG; ++i) {
+        const int place = (grp0 + g) * 16 + i * L::RPL + lane_row;
+        kc[g][i] = 16u * unsigned(lane_chunk ^ L::k_turn(place));
+        vc[g][i] = 16u * unsigned(lane_chunk ^ L::v_turn(place));
+      }
+    seek(t);
+  }
+  // To tile t.
+  __device__ __forceinline__ void seek(int t) {
+    const int hist = tl.nA + tl.nB;
+    is_new = t >= hist;
+    int last;                                            // last tile of the run
+    if (!is_new) {
+      k0 = (t < tl.nA ? t : tl.firstB + t - tl.nA) * KT;
+      last = t < tl.nA ? tl.nA : tl.firstB + tl.nB;
+    } else {
+      t -= hist;
+      k0 = (t < tl.nC ? t : tl.firstD + t - tl.nC) * KT;
+      last = t < tl.nC ? tl.nC : tl.firstD + tl.nD;
     }
-    load_group<D>(s, ko, vo, at, v_at);
+    end = last * KT;
+    look_up();
+  }
+  // By `step` tiles, onto tile t.
+  __device__ __forceinline__ void advance(int step, int t) {
+    k0 += step * KT;
+    if (__builtin_expect(k0 >= end, 0)) seek(t); else look_up();
+  }
+  __device__ __forceinline__ void look_up() {
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int row = k0 + 16 * (grp0 + g);
+      page[g] = !is_new && row < r.held ? pages[row >> p.page_log2] : 0;
+    }
+  }
+  // The tile's rows to LDS: K rows of the tile at `at`, V rows at `v_at`.
+  __device__ __forceinline__ void load(unsigned at, unsigned v_at) {
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int row = k0 + 16 * (grp0 + g);
+      const bool no_page = unsigned(page[g]) >= unsigned(p.n_pages);
+      bad |= no_page;
+      const int64_t in_pool = ((int64_t(no_page ? 0 : page[g]) << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * L::ROWB;
+      const int64_t in_new = int64_t(row) * p.kc_tok;
+      RowSource src;
+      src.k = is_new ? k_cur + in_new : p.k_pages + in_pool;
+      src.v = is_new ? v_cur + in_new : p.v_pages + in_pool;
+      src.stride = is_new ? p.kc_tok : unsigned(L::ROWB);
+      const int rows = clamp_int((is_new ? r.n : r.held) - row, 0, 16);
+      src.bytes = rows > 0 ? unsigned(rows - 1) * src.stride + L::ROWB : 0;
+      unsigned ko[L::LPG], vo[L::LPG];
+#pragma unroll
+      for (int i = 0; i < L::LPG; ++i) {
+        const unsigned first = unsigned(i * L::RPL + lane_row) * src.stride;
+        ko[i] = first + kc[g][i];
+        vo[i] = first + vc[g][i];
+      }
+      load_group<D>(src, ko, vo, at + (grp0 + g) * 16 * L::ROWB, v_at + (grp0 + g) * 16 * L::ROWB);
+    }
   }
 };
+
+// Keys that every row of a range sees, of the cache and of the new tokens: [0, a) and [b, c) (uniform).
+struct Free { int a, b, c; };
+struct FreeKeys {
+  Free hist, fresh;
+  // Key behind the last of the keys from k0 on that are seen without a gap, k0 itself or less if it is not.
+  __device__ __forceinline__ int until(int k0, bool is_new) const {
+    const int a = is_new ? fresh.a : hist.a, b = is_new ? fresh.b : hist.b, c = is_new ? fresh.c : hist.c;
+    return k0 < a ? a : k0 >= b ? c : k0;
+  }
+};
+__device__ __forceinline__ FreeKeys free_keys(const Request &r, const RowRange &x) {
+  FreeKeys f;
+  const Visible v = visible_slots(r, x.first1);
+  f.hist = Free{v.a1, v.b0, v.b1};
+  f.fresh = Free{clamp_int(r.s - r.L, 0, x.end0), max(0, x.first1 - r.w), x.end0};
+  return f;
+}
 
 // ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
 
@@ -431,14 +472,16 @@ struct Rows {
   static constexpr int KS = D / 32, DB = D / 16;
   s16x8 q[KS][QB];
   f32x4 o[DB][QB];
-  float m[QB], l[QB];
+  float m[QB], minus_mc[QB], l[QB];
+  bool all_set;              // every row of the wave has a reference (uniform)
   RowMask mask[QB];
 
   __device__ __forceinline__ void clear() {
+    all_set = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       m[qb] = -INFINITY;
-      l[qb] = 0.f;
+      minus_mc[qb] = l[qb] = 0.f;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -508,56 +551,85 @@ struct Rows {
       }
   }
 
-  // Weights of a tile, packed as the second product's operand; the reference moves up where a score is `slack` above it, so
-  // weights stay below 2^8 and moves are rare.
-  __device__ __forceinline__ void weights(const PagedParams &p, f32x4 (&s)[KB][QB], s16x8 (&w)[KB / 2][QB]) {
-    float top[QB];
-    bool up = false;
+  // Weights 2^(c s - c m) of row block qb, packed as the second product's operand, and their sum over the lane's keys.
+  __device__ __forceinline__ float weigh(const PagedParams &p, const f32x4 (&s)[KB][QB], int qb, s16x8 (&w)[KB / 2][QB]) const {
+    f32x4 sum;
+#pragma unroll
+    for (int ts = 0; ts < KB / 2; ++ts) {
+      u32x4 x;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x4 e;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) e[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * ts + u][qb][v], p.c, minus_mc[qb]));
+        sum = ts + u == 0 ? e : sum + e;
+        x[2 * u] = T::pack(e[0], e[1]);
+        x[2 * u + 1] = T::pack(e[2], e[3]);
+      }
+      w[ts][qb] = __builtin_bit_cast(s16x8, x);
+    }
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+
+  // The reference goes up to the largest score so far.
+  __device__ __forceinline__ void raise(const PagedParams &p, const f32x4 (&s)[KB][QB]) {
+    bool none = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      top[qb] = s[0][qb][0];
+      float t = s[0][qb][0];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) top[qb] = fmaxf(top[qb], s[kb][qb][v]);
-      up |= top[qb] > m[qb] + p.slack;                   // m = -inf: any score that is not
-    }
-    if (__builtin_amdgcn_ballot_w64(up)) {
+        for (int v = 0; v < 4; ++v) t = fmaxf(t, s[kb][qb][v]);
+      t = fmaxf(t, __shfl_xor(t, 16));
+      t = fmaxf(t, __shfl_xor(t, 32));
+      t = fmaxf(t, m[qb]);
+      // no score yet: the reference stays, and nothing is scaled by the NaN of inf - inf
+      const float scale = t == m[qb] ? 1.f : __builtin_amdgcn_exp2f((m[qb] - t) * p.c);
+      m[qb] = t;
+      minus_mc[qb] = t == -INFINITY ? 0.f : -(t * p.c);
+      l[qb] *= scale;
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        float t = top[qb];
-        t = fmaxf(t, __shfl_xor(t, 16));
-        t = fmaxf(t, __shfl_xor(t, 32));
-        t = fmaxf(t, m[qb]);
-        // no key with a score yet: the reference stays, and nothing is scaled by the NaN of inf - inf
-        const float scale = t == m[qb] ? 1.f : __builtin_amdgcn_exp2f((m[qb] - t) * p.c);
-        m[qb] = t;
-        l[qb] *= scale;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[db][qb] *= scale;
-      }
+      for (int db = 0; db < DB; ++db) o[db][qb] *= scale;
+      none |= t == -INFINITY;
     }
+    all_set = !__builtin_amdgcn_ballot_w64(none);
+  }
+
+  // The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
+  // lane's weights add up to more than 2^15 (fp16 holds the weights to 2^16, and sums and outputs stay far from the largest
+  // number in 32 bits), where a row has no reference yet, and where rows do not see all keys, the wave looks for the maximum,
+  // brings what it has to the new reference and weighs the tile (again): any_tile.  That leaves the common tile without a
+  // maximum, a comparison per score or a product of the outputs.
+  //
+  // A tile that every row sees, once all have a reference.  False, and nothing has changed, if it has to be taken by any_tile.
+  __device__ __forceinline__ bool seen_tile(const PagedParams &p, const char *k, const char *v) {
+    constexpr float kMost = 32768.f;
+    f32x4 s[KB][QB];
+    s16x8 w[KB / 2][QB];
+    float sum[QB];
+    scores(k, s);
+    bool over = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      const float mc = m[qb] == -INFINITY ? 0.f : m[qb] * p.c;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s[kb][qb][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][qb][v], p.c, -mc));
-      f32x4 sum = s[0][qb];
-#pragma unroll
-      for (int kb = 1; kb < KB; ++kb) sum += s[kb][qb];
-      l[qb] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-      for (int ts = 0; ts < KB / 2; ++ts) {
-        u32x4 x;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) x[2 * u + v] = T::pack(s[2 * ts + u][qb][2 * v], s[2 * ts + u][qb][2 * v + 1]);
-        w[ts][qb] = __builtin_bit_cast(s16x8, x);
-      }
+      sum[qb] = weigh(p, s, qb, w);
+      over |= !(sum[qb] <= kMost);
     }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(over) != 0, 0)) return false;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
+    values(v, w);
+    return true;
+  }
+  __device__ __forceinline__ void any_tile(const PagedParams &p, const Request &r, const char *k, const char *v, int k0, bool is_new, bool all_seen) {
+    f32x4 s[KB][QB];
+    s16x8 w[KB / 2][QB];
+    scores(k, s);
+    if (!all_seen) hide(r, k0, is_new, s);
+    raise(p, s);
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) l[qb] += weigh(p, s, qb, w);
+    values_hidden(v, w, all_seen);
   }
 
   __device__ __forceinline__ static s16x8 v_operand(const char *base, int turn, int ts, int db) {
@@ -586,7 +658,7 @@ struct Rows {
 
   // The same for a tile that some rows do not see all of.  A weight of zero does not hide an infinity or a NaN from the product, so
   // those take part as what they do to a row that sees them: three products of their indicators say which rows do.
-  __device__ __forceinline__ void values_hidden(const char *v, const s16x8 (&w)[KB / 2][QB]) {
+  __device__ __forceinline__ void values_hidden(const char *v, const s16x8 (&w)[KB / 2][QB], bool all_seen) {
     using L = Layout<D>;
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     const int row = 8 * g + (j >> 2), turn = L::v_turn(row) / 2;
@@ -600,7 +672,7 @@ struct Rows {
 #pragma unroll
         for (int k = 0; k < 8; ++k) odd |= (u16(a[k]) & T::kExponent) == T::kExponent;
       }
-    if (!__builtin_amdgcn_ballot_w64(odd)) return values(v, w);
+    if (__builtin_expect(all_seen || !__builtin_amdgcn_ballot_w64(odd), 1)) return values(v, w);
     const unsigned one_bits = T::pack(1.f, 1.f);
     const short one = short(one_bits);
 #pragma unroll 1
@@ -635,14 +707,6 @@ struct Rows {
       }
   }
 };
-
-// Whether every row of the range sees all KT keys from k0 on.
-template <int KT>
-__device__ __forceinline__ bool all_seen(const Request &r, const RowRange &x, const Visible &v, int k0, bool is_new) {
-  if (!is_new) return k0 + KT <= v.a1 || (k0 >= v.b0 && k0 + KT <= v.b1);
-  const int c1 = clamp_int(r.s - r.L, 0, x.end0);
-  return k0 + KT <= c1 || (k0 >= x.first1 - r.w && k0 + KT <= x.end0);
-}
 
 template <class T>
 __device__ __forceinline__ void store_row4(const PagedParams &p, const Request &r, int h, int row, int col, f32x4 x) {
@@ -691,37 +755,50 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
 
     Rows<T, D, KT / 16, 2> rows;
     rows.clear();
-    Loader<D> ld(p, r, un.b, un.h);
-    const Visible inner = visible_slots(r, x.first1);
-    const int row0 = un.row0 + 32 * wave;
+    Cursor<D, KT, 1> ld(p, r, tl, un.b, un.h, wave, t0);
+    const int row0 = un.row0 + 32 * wave, rows_left = r.n * p.G - row0;
     if (t0 < t1) {
-      bool is_new;
-      int k0 = tl.at(t0, is_new);
-      ld.load(k0 + 16 * wave, is_new, wave, lds0 + wave * 16 * L::ROWB, lds0 + TILE + wave * 16 * L::ROWB);
+      const RowRange mine = row_range(p, r, min(row0, r.n * p.G - 1), 32);
+      const FreeKeys seen = free_keys(r, mine);
+      ld.load(lds0, lds0 + TILE);
       rows.load_q(p, r, un.h, row0);
-      for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1;
-        // the wave's rows of this tile have landed, and every wave is done with the tile before
+      int k0 = ld.k0;
+      bool is_new = ld.is_new;
+      ld.advance(1, t0 + 1);
+      int buf = 2 * TILE;
+      // The wave's rows of the next tile have landed and every wave is done with the tile before: once per tile and wave.
+      int now_k0 = 0, t = t0;
+      bool now_new = false;
+      auto next = [&] {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        bool next_new = false;
-        int next_k0 = 0;
+        now_k0 = k0;
+        now_new = is_new;
+        k0 = ld.k0;
+        is_new = ld.is_new;
+        buf ^= 2 * TILE;
         if (t + 1 < t1) {
-          next_k0 = tl.at(t + 1, next_new);
-          const unsigned to = lds0 + (buf ^ 1) * 2 * TILE + wave * 16 * L::ROWB;
-          ld.load(next_k0 + 16 * wave, next_new, wave, to, to + TILE);
+          const unsigned to = lds0 + (buf ^ 2 * TILE);
+          ld.load(to, to + TILE);
+          ld.advance(1, t + 2);
         }
-        if (row0 < r.n * p.G) {
-          const char *k = tiles + buf * 2 * TILE, *v = k + TILE;
-          f32x4 s[KT / 16][2];
-          s16x8 w[KT / 32][2];
-          rows.scores(k, s);
-          const bool hidden = !all_seen<KT>(r, x, inner, k0, is_new);
-          if (hidden) rows.hide(r, k0, is_new, s);
-          rows.weights(p, s, w);
-          if (hidden) rows.values_hidden(v, w); else rows.values(v, w);
+      };
+      // a wave without rows, or whose rows see none of the tile, has nothing to do
+      auto idle = [&] { return rows_left <= 0 || (now_new && now_k0 >= mine.end1); };
+      auto all_seen = [&] { return now_k0 + KT <= seen.until(now_k0, now_new); };
+      while (t < t1) {
+        next();
+        bool due = true;
+        if (!idle()) {
+          while (rows.all_set && all_seen()) {           // the loop that takes the time
+            due = !rows.seen_tile(p, tiles + buf, tiles + buf + TILE);
+            if (due || t + 1 >= t1) break;
+            ++t;
+            next();
+            due = true;
+          }
+          if (due && !idle()) rows.any_tile(p, r, tiles + buf, tiles + buf + TILE, now_k0, now_new, all_seen());
         }
-        k0 = next_k0;
-        is_new = next_new;
+        ++t;
       }
     }
     if (ld.bad) poison = u;
@@ -793,37 +870,37 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
 
     Rows<T, D, 2, QB> rows;
     rows.clear();
-    Loader<D> ld(p, r, un.b, un.h);
-    const Visible inner = visible_slots(r, x.first1);
-    auto issue = [&](int t, int buf) {
-      bool is_new;
-      const int k0 = tl.at(t, is_new);
-      const unsigned to = lds0 + buf * 2 * TILE;
-#pragma unroll
-      for (int grp = 0; grp < 2; ++grp)
-        ld.load(k0 + 16 * grp, is_new, grp, to + grp * 16 * L::ROWB, to + TILE + grp * 16 * L::ROWB);
-    };
     int t = t0 + wave;
-    if (t < t1) issue(t, 0);
-    if (t + kFewWaves < t1) issue(t + kFewWaves, 1);
+    Cursor<D, KT, 2> ld(p, r, tl, un.b, un.h, 0, max(min(t, t1 - 1), 0));
+    const FreeKeys seen = free_keys(r, x);
+    // where the tiles that are under way begin
+    int k0[RING];
+    bool is_new[RING];
+#pragma unroll
+    for (int i = 0; i < RING; ++i) {
+      k0[i] = ld.k0;
+      is_new[i] = ld.is_new;
+      if (t + i * kFewWaves < t1) {
+        ld.load(lds0 + i * 2 * TILE, lds0 + i * 2 * TILE + TILE);
+        ld.advance(kFewWaves, t + (i + 1) * kFewWaves);
+      }
+    }
     rows.load_q(p, r, un.h, un.row0);
     for (int buf = 0; t < t1; t += kFewWaves, buf ^= 1) {
       // this tile has landed, the next one may still be on its way
       if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      bool is_new;
-      const int k0 = tl.at(t, is_new);
+      const int now_k0 = buf ? k0[1] : k0[0];
+      const bool now_new = buf ? is_new[1] : is_new[0];
       const char *k = &tiles[wave][buf][0][0], *v = &tiles[wave][buf][1][0];
-      f32x4 s[2][QB];
-      s16x8 w[1][QB];
-      rows.scores(k, s);
-      const bool hidden = !all_seen<KT>(r, x, inner, k0, is_new);
-      if (hidden) rows.hide(r, k0, is_new, s);
-      rows.weights(p, s, w);
-      if (hidden) rows.values_hidden(v, w); else rows.values(v, w);
+      const bool all_seen = now_k0 + KT <= seen.until(now_k0, now_new);
+      if (!(all_seen && rows.all_set && rows.seen_tile(p, k, v))) rows.any_tile(p, r, k, v, now_k0, now_new, all_seen);
       if (t + 2 * kFewWaves < t1) {
+        (buf ? k0[1] : k0[0]) = ld.k0;
+        (buf ? is_new[1] : is_new[0]) = ld.is_new;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the reads of this buffer are done
-        issue(t + 2 * kFewWaves, buf);
+        ld.load(lds0 + buf * 2 * TILE, lds0 + buf * 2 * TILE + TILE);
+        ld.advance(kFewWaves, t + 3 * kFewWaves);
       }
     }
     if (ld.bad) poison = u;
@@ -1015,7 +1092,6 @@ extern "C" df_status df_paged_attn(const df_paged_attn_args *a, void *stream) {
   p.units = int(units);
   p.c = a->softmax_scale * 1.4426950408889634f;
   p.ln_unit = float(double(a->softmax_scale) / double(p.c));
-  p.slack = 8.f / p.c;
   p.ws = static_cast<char *>(a->workspace);
   // the most tiles that a unit can have: its slots and its new tokens, each in two runs
   const int64_t slots = int64_t(c->max_pages) * c->page_tokens;
