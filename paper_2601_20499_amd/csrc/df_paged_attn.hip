@@ -37,6 +37,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
 typedef const __attribute__((address_space(4))) int const_int;
 
 struct Bf16 {
@@ -310,7 +311,7 @@ __device__ __forceinline__ unsigned scalar(unsigned x) { return unsigned(__built
 // Where a group of 16 rows comes from (uniform).
 struct RowSource {
   const char *k, *v;         // first row
-  unsigned stride, bytes;    // bytes between rows, addressable bytes (0: none; loads past them write zeros)
+  unsigned bytes;            // addressable bytes (0: none; loads past them write zeros)
 };
 
 // 16 rows of K and V into LDS, asynchronously: LPG loads each.  `at` is the LDS address of the K rows, the V rows lie `v_off` behind them.
@@ -352,60 +353,60 @@ __device__ __forceinline__ void load_group(const RowSource &src, const unsigned 
   }
 }
 
-// Walks the tiles of a unit in the order of Tiles, `ahead` of the tile that is computed, and brings their rows.  Uniform but for
-// the lane's offsets.  The page of the next tile's rows is looked up one step before it is used.
-template <int D, int KT, int GROUPS>                     // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
-struct Cursor {
+// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles.  Uniform but for the lane's offsets.  Whole tiles that
+// lie one behind the other are a run in which a step is a few scalar instructions; where a run begins (seek) everything about
+// it is worked out.  A tile's page is looked up one step before it is used.
+template <int D, int KT, int GROUPS, int STEP>           // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
+struct Feed {
   using L = Layout<D>;
   const PagedParams &p;
   const Request &r;
   const Tiles<KT> &tl;
   const int grp0;
   const_int *pages;          // the head's row of the block table
-  const char *k_cur, *v_cur; // the head's new tokens, the request's first row
-  int lane_row;              // row of a load's rows that the lane fetches
-  unsigned kc[GROUPS][L::LPG], vc[GROUPS][L::LPG];       // and its chunk's place in the source row, in bytes
-  int k0, end;               // first key of the tile, end of its run of tiles
+  const int64_t cur;         // byte offset of the request's first new token of the head
+  int t;                     // the tile that is brought next,
+  int k0;                    // its first key,
+  int left;                  // whole tiles from it on in its run, itself among them (a tile that is cut short counts as one)
   bool is_new;
   int page[GROUPS];
+  unsigned bytes[GROUPS];
+  unsigned ko[GROUPS][L::LPG], vo[GROUPS][L::LPG];       // the lane's 16 bytes of every load, from the group's first row on
   bool bad;                  // a page was no page of the pool
 
-  __device__ __forceinline__ Cursor(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, int b, int h, int grp0_, int t)
-      : p(p_), r(r_), tl(tl_), grp0(grp0_), lane_row((threadIdx.x & 63) / L::CH), bad(r_.bad) {
-    pages = p.table + (int64_t(b) * p.Hkv + h) * p.max_pages;
-    k_cur = p.k_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
-    v_cur = p.v_cur + int64_t(r.q0) * p.kc_tok + h * p.kc_head;
-    const int lane_chunk = (threadIdx.x & 63) % L::CH;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-      for (int i = 0; i < L::LPG; ++i) {
-        const int place = (grp0 + g) * 16 + i * L::RPL + lane_row;
-        kc[g][i] = 16u * unsigned(lane_chunk ^ L::k_turn(place));
-        vc[g][i] = 16u * unsigned(lane_chunk ^ L::v_turn(place));
-      }
-    seek(t);
+  __device__ __forceinline__ Feed(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, int b, int h, int grp0_, int t_)
+      : p(p_), r(r_), tl(tl_), grp0(grp0_), pages(p_.table + (int64_t(b) * p_.Hkv + h) * p_.max_pages),
+        cur(int64_t(r_.q0) * p_.kc_tok + h * p_.kc_head), t(t_), bad(r_.bad) {
+    seek();
   }
-  // To tile t.
-  __device__ __forceinline__ void seek(int t) {
+  __device__ __forceinline__ void seek() {
     const int hist = tl.nA + tl.nB;
-    is_new = t >= hist;
     int last;                                            // last tile of the run
+    is_new = t >= hist;
     if (!is_new) {
       k0 = (t < tl.nA ? t : tl.firstB + t - tl.nA) * KT;
       last = t < tl.nA ? tl.nA : tl.firstB + tl.nB;
     } else {
-      t -= hist;
-      k0 = (t < tl.nC ? t : tl.firstD + t - tl.nC) * KT;
-      last = t < tl.nC ? tl.nC : tl.firstD + tl.nD;
+      const int i = t - hist;
+      k0 = (i < tl.nC ? i : tl.firstD + i - tl.nC) * KT;
+      last = i < tl.nC ? tl.nC : tl.firstD + tl.nD;
     }
-    end = last * KT;
+    const int limit = is_new ? r.n : r.held;
+    left = max(1, min(last, limit / KT) - k0 / KT);
+    const unsigned stride = is_new ? p.kc_tok : unsigned(L::ROWB);
+    const int lane_row = (threadIdx.x & 63) / L::CH, lane_chunk = (threadIdx.x & 63) % L::CH;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int rows = clamp_int(limit - (k0 + 16 * (grp0 + g)), 0, 16);
+      bytes[g] = rows > 0 ? unsigned(rows - 1) * stride + L::ROWB : 0;
+#pragma unroll
+      for (int i = 0; i < L::LPG; ++i) {
+        const int row = i * L::RPL + lane_row, place = (grp0 + g) * 16 + row;
+        ko[g][i] = unsigned(row) * stride + 16u * unsigned(lane_chunk ^ L::k_turn(place));
+        vo[g][i] = unsigned(row) * stride + 16u * unsigned(lane_chunk ^ L::v_turn(place));
+      }
+    }
     look_up();
-  }
-  // By `step` tiles, onto tile t.
-  __device__ __forceinline__ void advance(int step, int t) {
-    k0 += step * KT;
-    if (__builtin_expect(k0 >= end, 0)) seek(t); else look_up();
   }
   __device__ __forceinline__ void look_up() {
 #pragma unroll
@@ -414,29 +415,29 @@ struct Cursor {
       page[g] = !is_new && row < r.held ? pages[row >> p.page_log2] : 0;
     }
   }
-  // The tile's rows to LDS: K rows of the tile at `at`, V rows at `v_at`.
-  __device__ __forceinline__ void load(unsigned at, unsigned v_at) {
+  // The tile's rows to LDS: K rows of the tile at `k_to`, V rows at `v_to`; then on by STEP tiles, if there is one before tile `end`.
+  __device__ __forceinline__ void bring(unsigned k_to, unsigned v_to, int end) {
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
       const int row = k0 + 16 * (grp0 + g);
-      const bool no_page = unsigned(page[g]) >= unsigned(p.n_pages);
-      bad |= no_page;
-      const int64_t in_pool = ((int64_t(no_page ? 0 : page[g]) << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * L::ROWB;
-      const int64_t in_new = int64_t(row) * p.kc_tok;
-      RowSource src;
-      src.k = is_new ? k_cur + in_new : p.k_pages + in_pool;
-      src.v = is_new ? v_cur + in_new : p.v_pages + in_pool;
-      src.stride = is_new ? p.kc_tok : unsigned(L::ROWB);
-      const int rows = clamp_int((is_new ? r.n : r.held) - row, 0, 16);
-      src.bytes = rows > 0 ? unsigned(rows - 1) * src.stride + L::ROWB : 0;
-      unsigned ko[L::LPG], vo[L::LPG];
-#pragma unroll
-      for (int i = 0; i < L::LPG; ++i) {
-        const unsigned first = unsigned(i * L::RPL + lane_row) * src.stride;
-        ko[i] = first + kc[g][i];
-        vo[i] = first + vc[g][i];
+      const char *k = p.k_pages, *v = p.v_pages;
+      int64_t at;
+      if (is_new) {
+        k = p.k_cur;
+        v = p.v_cur;
+        at = cur + int64_t(row) * p.kc_tok;
+      } else {
+        const bool no_page = unsigned(page[g]) >= unsigned(p.n_pages);
+        bad |= no_page;
+        at = ((int64_t(no_page ? 0 : page[g]) << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * L::ROWB;
       }
-      load_group<D>(src, ko, vo, at + (grp0 + g) * 16 * L::ROWB, v_at + (grp0 + g) * 16 * L::ROWB);
+      load_group<D>(RowSource{k + at, v + at, bytes[g]}, ko[g], vo[g], k_to + (grp0 + g) * 16 * L::ROWB, v_to + (grp0 + g) * 16 * L::ROWB);
+    }
+    t += STEP;
+    k0 += STEP * KT;
+    left -= STEP;
+    if (t < end) {
+      if (__builtin_expect(left <= 0, 0)) seek(); else look_up();
     }
   }
 };
@@ -461,20 +462,14 @@ __device__ __forceinline__ FreeKeys free_keys(const Request &r, const RowRange &
 
 // ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
 
-// The lane's row in each of its blocks of 16 rows, as masks need it.
-struct RowMask {
-  int lim_hist, lim_new;     // lowest position (window) that the row sees of the cache and of the new tokens
-  int end;                   // new tokens before this one
-};
-
 template <class T, int D, int KB, int QB>      // KB blocks of 16 keys, QB blocks of 16 rows
 struct Rows {
   static constexpr int KS = D / 32, DB = D / 16;
+  static constexpr int kAhead = 4;             // operands on their way from LDS
   s16x8 q[KS][QB];
   f32x4 o[DB][QB];
   float m[QB], minus_mc[QB], l[QB];
   bool all_set;              // every row of the wave has a reference (uniform)
-  RowMask mask[QB];
 
   __device__ __forceinline__ void clear() {
     all_set = false;
@@ -489,7 +484,7 @@ struct Rows {
 
   // The lane's share of rows row0 + 16 qb + lane % 16; rows behind the request's last repeat it and are not stored.
   __device__ __forceinline__ void load_q(const PagedParams &p, const Request &r, int h, int row0) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, block = min(p.block, max(r.n, 1));
+    const int lane = threadIdx.x & 63, g = lane >> 4;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int row = min(row0 + 16 * qb + (lane & 15), r.n * p.G - 1);
@@ -497,57 +492,83 @@ struct Rows {
       const char *src = p.q + int64_t(r.q0 + i) * p.q_tok + head * p.q_head + 16 * g;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) q[ks][qb] = *reinterpret_cast<const s16x8 *>(src + 64 * ks);
-      const int first = i / block * block;
-      mask[qb].end = min(first + block, r.n);
-      mask[qb].lim_new = first - r.w;
-      mask[qb].lim_hist = r.L + first - r.w;
     }
   }
 
-  // S^T: scores of keys 32 (kb / 2) + 8 g + 4 (kb % 2) + v of the lane's quarter g.
-  __device__ __forceinline__ void scores(const char *k, f32x4 (&s)[KB][QB]) const {
+  // Waits for the queries here, so that no wait for them is left in the loop over tiles (where it would also wait for tiles).
+  __device__ __forceinline__ void settle() {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) asm volatile("" : "+v"(q[ks][qb]));
+  }
+
+  // S^T: scores of keys 32 (kb / 2) + 8 g + 4 (kb % 2) + v of the lane's quarter g.  kAhead operands are on their way from LDS while
+  // the matrix core works: left to itself the compiler reads each right before its use and waits out the latency.
+  __device__ __forceinline__ void scores(unsigned k, f32x4 (&s)[KB][QB]) const {
     const int lane = threadIdx.x & 63, g = lane >> 4, mrow = lane & 15;
     using L = Layout<D>;
-    const char *base = k + key_of_operand_row(mrow, 0) * L::ROWB;
-    const int turn = L::k_turn(key_of_operand_row(mrow, 0));
+    const int row = key_of_operand_row(mrow, 0);
+    // chunk 4 ks + g of the row; tiles begin at multiples of 1 KB, so ks turns bits of the address
+    const unsigned first = k + unsigned(row * L::ROWB + 16 * (g ^ L::k_turn(row)));
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const char *at = base + 16 * ((4 * ks + g) ^ turn);
+      const unsigned at = first ^ unsigned(64 * ks);
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        const s16x8 a = *reinterpret_cast<const s16x8 *>(at + (32 * (kb >> 1) + 4 * (kb & 1)) * L::ROWB);
+        const s16x8 a = *(const lds_s16x8 *)(uintptr_t)(at + (32 * (kb >> 1) + 4 * (kb & 1)) * L::ROWB);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
           s[kb][qb] = T::mfma(a, q[ks][qb], ks ? s[kb][qb] : f32x4{0.f, 0.f, 0.f, 0.f});
       }
     }
+    // the order: kAhead reads, then a read behind every operand's products
+    constexpr int OPS = KS * KB, A = OPS < kAhead ? OPS : kAhead;
+    __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
+#pragma unroll
+    for (int i = 0; i < OPS - A; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, QB, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, A * QB, 0);
   }
 
+  // What the lane's rows see of a tile's keys.
+  struct Sight {
+    int lim[QB], end[QB];    // lowest position, and key behind the last one
+    int at;                  // slots of the ring in front of its oldest token
+    bool is_new, wrapped;
+    __device__ __forceinline__ Sight(const PagedParams &p, const Request &r, int row0, bool is_new_) : is_new(is_new_) {
+      const int lane = threadIdx.x & 63, block = min(p.block, max(r.n, 1)), turn = max(r.L - r.s, 0);
+      wrapped = turn > r.w;
+      at = wrapped && r.w > 0 ? turn % r.w : 0;
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const int row = min(row0 + 16 * qb + (lane & 15), r.n * p.G - 1), first = row / p.G / block * block;
+        lim[qb] = (is_new ? 0 : r.L) + first - r.w;
+        end[qb] = is_new ? min(first + block, r.n) : r.held;
+      }
+    }
+    // Position of a key, the largest one where windows do not matter.
+    __device__ __forceinline__ int position(const Request &r, int key) const {
+      if (is_new) return key < r.s - r.L ? INT32_MAX : key;
+      const int k = key - r.s;
+      return k < 0 ? INT32_MAX : wrapped ? r.L - at + k - (k < at ? 0 : r.w) : key;
+    }
+    __device__ __forceinline__ bool sees(int qb, int key, int pos) const { return key < end[qb] && pos >= lim[qb]; }
+  };
+
   // Scores of keys that a row does not see become minus infinity.
-  __device__ __forceinline__ void hide(const Request &r, int k0, bool is_new, f32x4 (&s)[KB][QB]) const {
+  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, int row0, int k0, bool is_new, f32x4 (&s)[KB][QB]) {
     const int g = (threadIdx.x & 63) >> 4;
-    const int turn = max(r.L - r.s, 0);
-    const bool wrapped = turn > r.w;
-    const int at = wrapped && r.w > 0 ? turn % r.w : 0;
+    const Sight sight(p, r, row0, is_new);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v;
-        int pos = key;                                   // position, or the largest where the window does not matter
-        if (is_new) {
-          if (key < r.s - r.L) pos = INT32_MAX;
-        } else if (key < r.s) {
-          pos = INT32_MAX;
-        } else if (wrapped) {
-          const int k = key - r.s;
-          pos = r.L - at + k - (k < at ? 0 : r.w);
-        }
+        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v, pos = sight.position(r, key);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          const bool seen = is_new ? key < mask[qb].end && pos >= mask[qb].lim_new : key < r.held && pos >= mask[qb].lim_hist;
-          s[kb][qb][v] = seen ? s[kb][qb][v] : -INFINITY;
-        }
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = sight.sees(qb, key, pos) ? s[kb][qb][v] : -INFINITY;
       }
   }
 
@@ -596,115 +617,116 @@ struct Rows {
     all_set = !__builtin_amdgcn_ballot_w64(none);
   }
 
-  // The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
-  // lane's weights add up to more than 2^15 (fp16 holds the weights to 2^16, and sums and outputs stay far from the largest
-  // number in 32 bits), where a row has no reference yet, and where rows do not see all keys, the wave looks for the maximum,
-  // brings what it has to the new reference and weighs the tile (again): any_tile.  That leaves the common tile without a
-  // maximum, a comparison per score or a product of the outputs.
-  //
-  // A tile that every row sees, once all have a reference.  False, and nothing has changed, if it has to be taken by any_tile.
-  __device__ __forceinline__ bool seen_tile(const PagedParams &p, const char *k, const char *v) {
+  // One tile.  The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
+  // lane's weights add up to more than 2^15 (fp16 holds weights to 2^16, and sums and outputs stay far from the largest number
+  // in 32 bits), and where a row has no reference yet, the wave looks for the maximum, brings what it has to the new reference
+  // and weighs the tile again.  That leaves the common tile without a maximum, a comparison per score or a product of the outputs.
+  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, int row0, unsigned k, unsigned v, int k0, bool is_new, bool all_seen) {
     constexpr float kMost = 32768.f;
     f32x4 s[KB][QB];
     s16x8 w[KB / 2][QB];
     float sum[QB];
     scores(k, s);
+    if (__builtin_expect(!all_seen, 0)) hide(p, r, row0, k0, is_new, s);
+    Values x = begin_values(v);
     bool over = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       sum[qb] = weigh(p, s, qb, w);
       over |= !(sum[qb] <= kMost);
     }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(over) != 0, 0)) return false;
+    if (__builtin_expect(!all_set || __builtin_amdgcn_ballot_w64(over), 0)) {
+      raise(p, s);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) sum[qb] = weigh(p, s, qb, w);
+    }
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
-    values(v, w);
-    return true;
-  }
-  __device__ __forceinline__ void any_tile(const PagedParams &p, const Request &r, const char *k, const char *v, int k0, bool is_new, bool all_seen) {
-    f32x4 s[KB][QB];
-    s16x8 w[KB / 2][QB];
-    scores(k, s);
-    if (!all_seen) hide(r, k0, is_new, s);
-    raise(p, s);
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) l[qb] += weigh(p, s, qb, w);
-    values_hidden(v, w, all_seen);
+    if (__builtin_expect(!all_seen && odd_values(v), 0)) odd_products(p, r, row0, v, k0, is_new, w); else values(x, w);
   }
 
-  __device__ __forceinline__ static s16x8 v_operand(const char *base, int turn, int ts, int db) {
+  // Where the lane reads V^T of a tile at `v`: columns 16 db + lane % 16 of keys 8 g .. 8 g + 3 and, four rows on, the next four.
+  __device__ __forceinline__ static unsigned v_first(unsigned v) {
     using L = Layout<D>;
-    const char *at = base + 32 * (db ^ turn) + 32 * ts * L::ROWB;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * L::ROWB));
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, row = 8 * g + (j >> 2);
+    return v + unsigned(row * L::ROWB + 16 * L::v_turn(row) + 8 * (j & 3));
+  }
+  __device__ __forceinline__ static s16x8 v_operand(unsigned first, int ts, int db) {
+    using L = Layout<D>;
+    const unsigned at = (first ^ unsigned(32 * db)) + 32 * ts * L::ROWB;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(at + 4 * L::ROWB));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 
-  // O^T += V^T P^T.
-  __device__ __forceinline__ void values(const char *v, const s16x8 (&w)[KB / 2][QB]) {
-    using L = Layout<D>;
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-    const int row = 8 * g + (j >> 2), turn = L::v_turn(row) / 2;
-    const char *base = v + row * L::ROWB + 8 * (j & 3);
+  // O^T += V^T P^T.  The first kAhead operands may be read before the weights are there (begin), the others follow as many operands ahead of
+  // their products.  (The order is the statements': the compiler does not move these reads.)
+  static constexpr int kValueOps = KB / 2 * DB, kValuesAhead = kValueOps < kAhead ? kValueOps : kAhead;
+  struct Values {
+    unsigned first;
+    s16x8 a[kValuesAhead];
+  };
+  __device__ __forceinline__ static Values begin_values(unsigned v) {
+    Values x;
+    x.first = v_first(v);
 #pragma unroll
-    for (int ts = 0; ts < KB / 2; ++ts)
+    for (int i = 0; i < kValuesAhead; ++i) x.a[i] = v_operand(x.first, i / DB, i % DB);
+    return x;
+  }
+  __device__ __forceinline__ void values(Values &x, const s16x8 (&w)[KB / 2][QB]) {
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const s16x8 a = v_operand(base, turn, ts, db);
+    for (int i = 0; i < kValueOps; ++i) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) o[db][qb] = T::mfma(a, w[ts][qb], o[db][qb]);
-      }
+      for (int qb = 0; qb < QB; ++qb) o[i % DB][qb] = T::mfma(x.a[i % kValuesAhead], w[i / DB][qb], o[i % DB][qb]);
+      if (i + kValuesAhead < kValueOps) x.a[i % kValuesAhead] = v_operand(x.first, (i + kValuesAhead) / DB, (i + kValuesAhead) % DB);
+    }
   }
 
-  // The same for a tile that some rows do not see all of.  A weight of zero does not hide an infinity or a NaN from the product, so
-  // those take part as what they do to a row that sees them: three products of their indicators say which rows do.
-  __device__ __forceinline__ void values_hidden(const char *v, const s16x8 (&w)[KB / 2][QB], bool all_seen) {
+  // A weight of zero does not hide an infinity or a NaN from the product.  Where some rows do not see all of a tile (only there) the wave
+  // looks for them among the values.  If there are any, the product takes zeros in their place, and each is added to the outputs of the rows that see
+  // its key: what an infinity or a NaN times a weight adds.
+  __device__ __forceinline__ static bool odd_values(unsigned v) {
+    typedef u16 u16x8 __attribute__((ext_vector_type(8)));
+    const unsigned first = v_first(v);
+    u16x8 top = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kValueOps; ++i)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x8, v_operand(first, i / DB, i % DB)) & u16(0x7fff));
+    u16 most = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = most > top[k] ? most : top[k];
+    return __builtin_amdgcn_ballot_w64(most >= T::kExponent) != 0;
+  }
+  __device__ __forceinline__ void odd_products(const PagedParams &p, const Request &r, int row0, unsigned v, int k0, bool is_new, const s16x8 (&w)[KB / 2][QB]) {
     using L = Layout<D>;
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-    const int row = 8 * g + (j >> 2), turn = L::v_turn(row) / 2;
-    const char *base = v + row * L::ROWB + 8 * (j & 3);
-    bool odd = false;
+    const unsigned first = v_first(v);
 #pragma unroll
-    for (int ts = 0; ts < KB / 2; ++ts)
+    for (int i = 0; i < kValueOps; ++i) {
+      s16x8 a = v_operand(first, i / DB, i % DB);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const s16x8 a = v_operand(base, turn, ts, db);
+      for (int k = 0; k < 8; ++k) a[k] = (u16(a[k]) & T::kExponent) == T::kExponent ? short(0) : a[k];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) odd |= (u16(a[k]) & T::kExponent) == T::kExponent;
-      }
-    if (__builtin_expect(all_seen || !__builtin_amdgcn_ballot_w64(odd), 1)) return values(v, w);
-    const unsigned one_bits = T::pack(1.f, 1.f);
-    const short one = short(one_bits);
+      for (int qb = 0; qb < QB; ++qb) o[i % DB][qb] = T::mfma(a, w[i / DB][qb], o[i % DB][qb]);
+    }
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const Sight sight(p, r, row0, is_new);
 #pragma unroll 1
-    for (int ts = 0; ts < KB / 2; ++ts)
+    for (int key = 0; key < 16 * KB; ++key) {
+      const int pos = sight.position(r, k0 + key);
+      const unsigned row = v + unsigned(key * L::ROWB);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const s16x8 a = v_operand(base, turn, ts, db);
-        s16x8 fin, pos, neg, nan;
+        // columns 16 db + 4 g .. + 3 of the key's row: half of chunk 2 db + g / 2
+        const s16x4 x = *(const lds_s16x4 *)(uintptr_t)(row + 16u * unsigned((2 * db + (g >> 1)) ^ L::v_turn(key)) + 8u * unsigned(g & 1));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const u16 x = u16(a[k]);
-          const bool f = (x & T::kExponent) != T::kExponent;
-          fin[k] = f ? a[k] : short(0);
-          pos[k] = x == T::kExponent ? one : short(0);
-          neg[k] = x == (T::kExponent | 0x8000u) ? one : short(0);
-          nan[k] = !f && (x & 0x7fffu) != T::kExponent ? one : short(0);
-        }
+        for (int i = 0; i < 4; ++i) {
+          const bool odd = (u16(x[i]) & T::kExponent) == T::kExponent;
+          const float f = odd ? ((u16(x[i]) & ~(T::kExponent | 0x8000u)) ? NAN : (u16(x[i]) & 0x8000u) ? -INFINITY : INFINITY) : 0.f;
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
-          const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-          const s16x8 b = ts == 0 ? w[0][qb] : w[KB / 2 - 1][qb];
-          const f32x4 up = T::mfma(pos, b, zero), down = T::mfma(neg, b, zero), none = T::mfma(nan, b, zero);
-          f32x4 x = T::mfma(fin, b, o[db][qb]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (up[i] != 0.f) x[i] += INFINITY;
-            if (down[i] != 0.f) x[i] -= INFINITY;
-            if (none[i] != 0.f) x[i] = NAN;
-          }
-          o[db][qb] = x;
+          for (int qb = 0; qb < QB; ++qb) o[db][qb][i] += sight.sees(qb, k0 + key, pos) ? f : 0.f;
         }
       }
+    }
   }
 };
 
@@ -755,50 +777,30 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
 
     Rows<T, D, KT / 16, 2> rows;
     rows.clear();
-    Cursor<D, KT, 1> ld(p, r, tl, un.b, un.h, wave, t0);
-    const int row0 = un.row0 + 32 * wave, rows_left = r.n * p.G - row0;
+    Feed<D, KT, 1, 1> ld(p, r, tl, un.b, un.h, wave, t0);
+    const int row0 = un.row0 + 32 * wave;
     if (t0 < t1) {
       const RowRange mine = row_range(p, r, min(row0, r.n * p.G - 1), 32);
       const FreeKeys seen = free_keys(r, mine);
-      ld.load(lds0, lds0 + TILE);
-      rows.load_q(p, r, un.h, row0);
+      // a wave without rows, or whose rows see none of the tile, has nothing to do
+      const int end_new = row0 < r.n * p.G ? mine.end1 : 0, end_hist = row0 < r.n * p.G ? INT32_MAX : 0;
       int k0 = ld.k0;
       bool is_new = ld.is_new;
-      ld.advance(1, t0 + 1);
-      int buf = 2 * TILE;
-      // The wave's rows of the next tile have landed and every wave is done with the tile before: once per tile and wave.
-      int now_k0 = 0, t = t0;
-      bool now_new = false;
-      auto next = [&] {
+      ld.bring(lds0, lds0 + TILE, t1);
+      rows.load_q(p, r, un.h, row0);
+      rows.settle();
+      unsigned buf = lds0;
+      for (int t = t0; t < t1; ++t) {
+        // the wave's rows of this tile have landed, and every wave is done with the tile before
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        now_k0 = k0;
-        now_new = is_new;
-        k0 = ld.k0;
-        is_new = ld.is_new;
-        buf ^= 2 * TILE;
-        if (t + 1 < t1) {
-          const unsigned to = lds0 + (buf ^ 2 * TILE);
-          ld.load(to, to + TILE);
-          ld.advance(1, t + 2);
-        }
-      };
-      // a wave without rows, or whose rows see none of the tile, has nothing to do
-      auto idle = [&] { return rows_left <= 0 || (now_new && now_k0 >= mine.end1); };
-      auto all_seen = [&] { return now_k0 + KT <= seen.until(now_k0, now_new); };
-      while (t < t1) {
-        next();
-        bool due = true;
-        if (!idle()) {
-          while (rows.all_set && all_seen()) {           // the loop that takes the time
-            due = !rows.seen_tile(p, tiles + buf, tiles + buf + TILE);
-            if (due || t + 1 >= t1) break;
-            ++t;
-            next();
-            due = true;
-          }
-          if (due && !idle()) rows.any_tile(p, r, tiles + buf, tiles + buf + TILE, now_k0, now_new, all_seen());
-        }
-        ++t;
+        const unsigned other = buf == lds0 ? lds0 + 2 * TILE : lds0;
+        const int next_k0 = ld.k0;
+        const bool next_new = ld.is_new;
+        if (t + 1 < t1) ld.bring(other, other + TILE, t1);
+        if (k0 < (is_new ? end_new : end_hist)) rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, k0 + KT <= seen.until(k0, is_new));
+        k0 = next_k0;
+        is_new = next_new;
+        buf = other;
       }
     }
     if (ld.bad) poison = u;
@@ -871,37 +873,33 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
     Rows<T, D, 2, QB> rows;
     rows.clear();
     int t = t0 + wave;
-    Cursor<D, KT, 2> ld(p, r, tl, un.b, un.h, 0, max(min(t, t1 - 1), 0));
+    Feed<D, KT, 2, kFewWaves> ld(p, r, tl, un.b, un.h, 0, max(min(t, t1 - 1), 0));
     const FreeKeys seen = free_keys(r, x);
-    // where the tiles that are under way begin
-    int k0[RING];
-    bool is_new[RING];
-#pragma unroll
-    for (int i = 0; i < RING; ++i) {
-      k0[i] = ld.k0;
-      is_new[i] = ld.is_new;
-      if (t + i * kFewWaves < t1) {
-        ld.load(lds0 + i * 2 * TILE, lds0 + i * 2 * TILE + TILE);
-        ld.advance(kFewWaves, t + (i + 1) * kFewWaves);
-      }
+    // where the tiles that are under way begin: this one's and the next one's
+    int k0 = ld.k0, next_k0 = 0;
+    bool is_new = ld.is_new, next_new = false;
+    if (t < t1) ld.bring(lds0, lds0 + TILE, t1);
+    if (t + kFewWaves < t1) {
+      next_k0 = ld.k0;
+      next_new = ld.is_new;
+      ld.bring(lds0 + 2 * TILE, lds0 + 3 * TILE, t1);
     }
     rows.load_q(p, r, un.h, un.row0);
-    for (int buf = 0; t < t1; t += kFewWaves, buf ^= 1) {
+    rows.settle();
+    for (unsigned buf = lds0; t < t1; t += kFewWaves) {
       // this tile has landed, the next one may still be on its way
       if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const int now_k0 = buf ? k0[1] : k0[0];
-      const bool now_new = buf ? is_new[1] : is_new[0];
-      const char *k = &tiles[wave][buf][0][0], *v = &tiles[wave][buf][1][0];
-      const bool all_seen = now_k0 + KT <= seen.until(now_k0, now_new);
-      if (!(all_seen && rows.all_set && rows.seen_tile(p, k, v))) rows.any_tile(p, r, k, v, now_k0, now_new, all_seen);
+      rows.tile(p, r, un.row0, buf, buf + TILE, k0, is_new, k0 + KT <= seen.until(k0, is_new));
+      k0 = next_k0;
+      is_new = next_new;
       if (t + 2 * kFewWaves < t1) {
-        (buf ? k0[1] : k0[0]) = ld.k0;
-        (buf ? is_new[1] : is_new[0]) = ld.is_new;
+        next_k0 = ld.k0;
+        next_new = ld.is_new;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the reads of this buffer are done
-        ld.load(lds0 + buf * 2 * TILE, lds0 + buf * 2 * TILE + TILE);
-        ld.advance(kFewWaves, t + 3 * kFewWaves);
+        ld.bring(buf, buf + TILE, t1);
       }
+      buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
     }
     if (ld.bad) poison = u;
     // the four waves' sums meet in LDS: references, row sums, outputs
