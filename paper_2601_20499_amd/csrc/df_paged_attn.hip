@@ -353,9 +353,9 @@ __device__ __forceinline__ void load_group(const RowSource &src, const unsigned 
   }
 }
 
-// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles.  Uniform but for the lane's offsets.  Whole tiles that
-// lie one behind the other are a run in which a step is a few scalar instructions; where a run begins (seek) everything about
-// it is worked out.  A tile's page is looked up one step before it is used.
+// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles.  Uniform but for what lies in lanes.  Tiles that lie
+// one behind the other are a run; where one begins (and every 64 tiles) seek looks up where the rows of the next 64 tiles lie, a
+// tile to a lane, so that a step has only to read a lane.
 template <int D, int KT, int GROUPS, int STEP>           // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
 struct Feed {
   using L = Layout<D>;
@@ -367,10 +367,13 @@ struct Feed {
   const int64_t cur;         // byte offset of the request's first new token of the head
   int t;                     // the tile that is brought next,
   int k0;                    // its first key,
-  int left;                  // whole tiles from it on in its run, itself among them (a tile that is cut short counts as one)
+  int left, whole;           // tiles and whole tiles from it on in its run, itself among them,
+  int lane;                  // and where its rows are noted
   bool is_new;
-  int page[GROUPS];
-  unsigned bytes[GROUPS];
+  const char *kb, *vb;       // row 0
+  unsigned stride;           // bytes between rows
+  int limit;                 // keys that are there
+  unsigned slots[GROUPS];    // lane i: the first row of tile t + STEP i's group
   unsigned ko[GROUPS][L::LPG], vo[GROUPS][L::LPG];       // the lane's 16 bytes of every load, from the group's first row on
   bool bad;                  // a page was no page of the pool
 
@@ -380,8 +383,8 @@ struct Feed {
     seek();
   }
   __device__ __forceinline__ void seek() {
-    const int hist = tl.nA + tl.nB;
-    int last;                                            // last tile of the run
+    const int hist = tl.nA + tl.nB, me = threadIdx.x & 63;
+    int last;                                            // tile behind the run's last
     is_new = t >= hist;
     if (!is_new) {
       k0 = (t < tl.nA ? t : tl.firstB + t - tl.nA) * KT;
@@ -391,55 +394,52 @@ struct Feed {
       k0 = (i < tl.nC ? i : tl.firstD + i - tl.nC) * KT;
       last = i < tl.nC ? tl.nC : tl.firstD + tl.nD;
     }
-    const int limit = is_new ? r.n : r.held;
-    left = max(1, min(last, limit / KT) - k0 / KT);
-    const unsigned stride = is_new ? p.kc_tok : unsigned(L::ROWB);
-    const int lane_row = (threadIdx.x & 63) / L::CH, lane_chunk = (threadIdx.x & 63) % L::CH;
+    limit = is_new ? r.n : r.held;
+    left = last - k0 / KT;
+    whole = min(last, limit / KT) - k0 / KT;
+    lane = 0;
+    stride = is_new ? p.kc_tok : unsigned(L::ROWB);
+    kb = is_new ? p.k_cur + cur : p.k_pages;
+    vb = is_new ? p.v_cur + cur : p.v_pages;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int rows = clamp_int(limit - (k0 + 16 * (grp0 + g)), 0, 16);
-      bytes[g] = rows > 0 ? unsigned(rows - 1) * stride + L::ROWB : 0;
+      const int row = k0 + me * (STEP * KT) + 16 * (grp0 + g);
+      slots[g] = is_new ? row : 0;
+      if (!is_new && me * STEP < left && row < limit) {
+        const int page = pages[row >> p.page_log2];
+        const bool is_page = unsigned(page) < unsigned(p.n_pages);
+        bad |= !is_page;
+        slots[g] = is_page ? (unsigned(page) << p.page_log2) + unsigned(row & ((1 << p.page_log2) - 1)) : 0;
+      }
 #pragma unroll
       for (int i = 0; i < L::LPG; ++i) {
-        const int row = i * L::RPL + lane_row, place = (grp0 + g) * 16 + row;
-        ko[g][i] = unsigned(row) * stride + 16u * unsigned(lane_chunk ^ L::k_turn(place));
-        vo[g][i] = unsigned(row) * stride + 16u * unsigned(lane_chunk ^ L::v_turn(place));
+        const int in_group = i * L::RPL + me / L::CH, place = (grp0 + g) * 16 + in_group;
+        ko[g][i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::k_turn(place));
+        vo[g][i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::v_turn(place));
       }
-    }
-    look_up();
-  }
-  __device__ __forceinline__ void look_up() {
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-      const int row = k0 + 16 * (grp0 + g);
-      page[g] = !is_new && row < r.held ? pages[row >> p.page_log2] : 0;
     }
   }
   // The tile's rows to LDS: K rows of the tile at `k_to`, V rows at `v_to`; then on by STEP tiles, if there is one before tile `end`.
   __device__ __forceinline__ void bring(unsigned k_to, unsigned v_to, int end) {
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int row = k0 + 16 * (grp0 + g);
-      const char *k = p.k_pages, *v = p.v_pages;
-      int64_t at;
-      if (is_new) {
-        k = p.k_cur;
-        v = p.v_cur;
-        at = cur + int64_t(row) * p.kc_tok;
-      } else {
-        const bool no_page = unsigned(page[g]) >= unsigned(p.n_pages);
-        bad |= no_page;
-        at = ((int64_t(no_page ? 0 : page[g]) << p.page_log2) + (row & ((1 << p.page_log2) - 1))) * L::ROWB;
-      }
-      load_group<D>(RowSource{k + at, v + at, bytes[g]}, ko[g], vo[g], k_to + (grp0 + g) * 16 * L::ROWB, v_to + (grp0 + g) * 16 * L::ROWB);
+      const int rows = clamp_int(limit - (k0 + 16 * (grp0 + g)), 0, 16);
+      const uint64_t at = uint64_t(unsigned(__builtin_amdgcn_readlane(int(slots[g]), lane))) * stride;
+      const unsigned bytes = rows > 0 ? unsigned(rows - 1) * stride + L::ROWB : 0;
+      load_group<D>(RowSource{kb + at, vb + at, bytes}, ko[g], vo[g], k_to + (grp0 + g) * 16 * L::ROWB, v_to + (grp0 + g) * 16 * L::ROWB);
     }
-    t += STEP;
-    k0 += STEP * KT;
-    left -= STEP;
-    if (t < end) {
-      if (__builtin_expect(left <= 0, 0)) seek(); else look_up();
-    }
+    on(1, end);
   }
+  __device__ __forceinline__ void on(int steps, int end) {
+    t += STEP * steps;
+    k0 += STEP * steps * KT;
+    left -= STEP * steps;
+    whole -= STEP * steps;
+    lane += steps;
+    if (__builtin_expect(t < end && (left <= 0 || lane >= 64), 0)) seek();
+  }
+  // Whether a page of the wave's was none, in any lane.
+  __device__ __forceinline__ bool met_bad() const { return __builtin_amdgcn_ballot_w64(bad) != 0; }
 };
 
 // Keys that every row of a range sees, of the cache and of the new tokens: [0, a) and [b, c) (uniform).
@@ -465,6 +465,7 @@ __device__ __forceinline__ FreeKeys free_keys(const Request &r, const RowRange &
 template <class T, int D, int KB, int QB>      // KB blocks of 16 keys, QB blocks of 16 rows
 struct Rows {
   static constexpr int KS = D / 32, DB = D / 16;
+  static constexpr float kMost = 32768.f;
   static constexpr int kAhead = 4;             // operands on their way from LDS
   s16x8 q[KS][QB];
   f32x4 o[DB][QB];
@@ -503,14 +504,18 @@ struct Rows {
       for (int qb = 0; qb < QB; ++qb) asm volatile("" : "+v"(q[ks][qb]));
   }
 
+  // Where the lane reads K of a tile at `k`: chunk 4 ks + lane / 16 of its operand row, for ks = 0.  (Tiles begin at multiples of 1 KB, so
+  // ks turns bits of the address.)
+  __device__ __forceinline__ static unsigned k_first(unsigned k) {
+    const int lane = threadIdx.x & 63, row = key_of_operand_row(lane & 15, 0);
+    return k + unsigned(row * Layout<D>::ROWB + 16 * ((lane >> 4) ^ Layout<D>::k_turn(row)));
+  }
+
   // S^T: scores of keys 32 (kb / 2) + 8 g + 4 (kb % 2) + v of the lane's quarter g.  kAhead operands are on their way from LDS while
   // the matrix core works: left to itself the compiler reads each right before its use and waits out the latency.
   __device__ __forceinline__ void scores(unsigned k, f32x4 (&s)[KB][QB]) const {
-    const int lane = threadIdx.x & 63, g = lane >> 4, mrow = lane & 15;
     using L = Layout<D>;
-    const int row = key_of_operand_row(mrow, 0);
-    // chunk 4 ks + g of the row; tiles begin at multiples of 1 KB, so ks turns bits of the address
-    const unsigned first = k + unsigned(row * L::ROWB + 16 * (g ^ L::k_turn(row)));
+    const unsigned first = k_first(k);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const unsigned at = first ^ unsigned(64 * ks);
@@ -558,8 +563,8 @@ struct Rows {
     __device__ __forceinline__ bool sees(int qb, int key, int pos) const { return key < end[qb] && pos >= lim[qb]; }
   };
 
-  // Scores of keys that a row does not see become minus infinity.
-  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, int row0, int k0, bool is_new, f32x4 (&s)[KB][QB]) {
+  // Scores of keys that a row does not see, and of those before `from`, become minus infinity.
+  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, int row0, int k0, bool is_new, int from, f32x4 (&s)[KB][QB]) {
     const int g = (threadIdx.x & 63) >> 4;
     const Sight sight(p, r, row0, is_new);
 #pragma unroll
@@ -568,7 +573,7 @@ struct Rows {
       for (int v = 0; v < 4; ++v) {
         const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v, pos = sight.position(r, key);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = sight.sees(qb, key, pos) ? s[kb][qb][v] : -INFINITY;
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = key >= from && sight.sees(qb, key, pos) ? s[kb][qb][v] : -INFINITY;
       }
   }
 
@@ -617,17 +622,16 @@ struct Rows {
     all_set = !__builtin_amdgcn_ballot_w64(none);
   }
 
-  // One tile.  The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
+  // One tile, or what of it begins at key `from`.  The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
   // lane's weights add up to more than 2^15 (fp16 holds weights to 2^16, and sums and outputs stay far from the largest number
   // in 32 bits), and where a row has no reference yet, the wave looks for the maximum, brings what it has to the new reference
   // and weighs the tile again.  That leaves the common tile without a maximum, a comparison per score or a product of the outputs.
-  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, int row0, unsigned k, unsigned v, int k0, bool is_new, bool all_seen) {
-    constexpr float kMost = 32768.f;
+  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, int row0, unsigned k, unsigned v, int k0, bool is_new, int from, bool all_seen) {
     f32x4 s[KB][QB];
     s16x8 w[KB / 2][QB];
     float sum[QB];
     scores(k, s);
-    if (__builtin_expect(!all_seen, 0)) hide(p, r, row0, k0, is_new, s);
+    if (__builtin_expect(!all_seen, 0)) hide(p, r, row0, k0, is_new, from, s);
     Values x = begin_values(v);
     bool over = false;
 #pragma unroll
@@ -750,6 +754,51 @@ __device__ __forceinline__ void store_lse(const PagedParams &p, const Request &r
 
 constexpr int kManyRows = 128, kManyKeys = 64;
 
+// What the loop over whole tiles that all rows of the wave see needs besides the queries.
+template <int D>
+struct SeenTiles {
+  unsigned k[D / 32], v[D / 16];                         // per lane: LDS addresses of the operands in buffer 0
+  unsigned ko[D / 32], vo[D / 32], slots;                // per lane, as in Feed
+  unsigned klo, khi, vlo, vhi, stride, bytes;            // row 0 of the run, bytes between rows, bytes of 16 rows
+  unsigned to;                                           // LDS address of the wave's K rows in buffer 0
+  int buf;                                               // buffer of the first tile
+  float c, most;
+  __device__ __forceinline__ void place(unsigned lds0, int buf_, int wave, float c_) {
+    constexpr int TILE = kManyKeys * Layout<D>::ROWB;
+    using R = Rows<Bf16, D, 4, 2>;                       // (the addresses do not depend on the type)
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) k[ks] = R::k_first(lds0) ^ unsigned(64 * ks);
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) v[db] = R::v_first(lds0 + TILE) ^ unsigned(32 * db);
+    to = scalar(lds0 + wave * 16 * Layout<D>::ROWB);
+    buf = scalar(buf_);
+    c = c_;
+    most = R::kMost;
+  }
+  template <class F>
+  __device__ __forceinline__ void rows_of(const F &f) {
+    const uint64_t ka = reinterpret_cast<uint64_t>(f.kb), va = reinterpret_cast<uint64_t>(f.vb);
+    klo = scalar(unsigned(ka));
+    khi = scalar(unsigned(ka >> 32));
+    vlo = scalar(unsigned(va));
+    vhi = scalar(unsigned(va >> 32));
+    stride = scalar(f.stride);
+    bytes = scalar(15 * f.stride + Layout<D>::ROWB);
+    slots = f.slots[0];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      ko[i] = f.ko[0][i];
+      vo[i] = f.vo[0][i];
+    }
+  }
+};
+// Up to n tiles from the one that is on its way to buffer a.buf, each as Rows::tile does it; lane i of a.slots is the tile behind the first.  Returns 0, or
+// 1 (2) where the tile of the last step, or its second half, is left to Rows::tile because its weights are too large.
+template <class T, int D>
+__device__ __forceinline__ int seen_tiles(const SeenTiles<D> &a, const s16x8 (&q)[D / 32][2], f32x4 (&o)[D / 16][2], float (&l)[2], const float (&nm)[2],
+                                          int &i, int n);
+#include "df_paged_tiles.inc"
+
 template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedParams p) {
   using L = Layout<D>;
@@ -791,19 +840,41 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
       rows.settle();
       unsigned buf = lds0;
       for (int t = t0; t < t1; ++t) {
+        if (rows.all_set && ld.is_new == is_new && ld.k0 == k0 + KT && k0 < (is_new ? end_new : end_hist)) {
+          // tiles that all rows see, the one behind each a whole one of the same run
+          const int until = seen.until(k0, is_new), n = min(min((until - k0) / KT, ld.whole), min(t1 - 1 - t, 64 - ld.lane));
+          if (n > 0) {
+            SeenTiles<D> a;
+            a.place(lds0, buf == lds0 ? 0 : 1, wave, p.c);
+            a.rows_of(ld);
+            int lane_at = scalar(ld.lane);
+            const int due = seen_tiles<T, D>(a, rows.q, rows.o, rows.l, rows.minus_mc, lane_at, scalar(n));
+            const int begun = lane_at - ld.lane, done = begun - (due != 0);
+            ld.on(begun, t1);
+            t += done;
+            k0 += done * KT;
+            if (done & 1) buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
+            if (due) {
+              rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, due == 1 ? k0 : k0 + KT / 2, due == 1);
+              k0 += KT;
+              buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
+              continue;
+            }
+          }
+        }
         // the wave's rows of this tile have landed, and every wave is done with the tile before
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         const unsigned other = buf == lds0 ? lds0 + 2 * TILE : lds0;
         const int next_k0 = ld.k0;
         const bool next_new = ld.is_new;
         if (t + 1 < t1) ld.bring(other, other + TILE, t1);
-        if (k0 < (is_new ? end_new : end_hist)) rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, k0 + KT <= seen.until(k0, is_new));
+        if (k0 < (is_new ? end_new : end_hist)) rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, k0, k0 + KT <= seen.until(k0, is_new));
         k0 = next_k0;
         is_new = next_new;
         buf = other;
       }
     }
-    if (ld.bad) poison = u;
+    if (ld.met_bad()) poison = u;
     __syncthreads();                     // all waves are done with the tiles and have said what pages they met
     const bool nan = poison == u;
 #pragma unroll
@@ -890,7 +961,7 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
       // this tile has landed, the next one may still be on its way
       if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      rows.tile(p, r, un.row0, buf, buf + TILE, k0, is_new, k0 + KT <= seen.until(k0, is_new));
+      rows.tile(p, r, un.row0, buf, buf + TILE, k0, is_new, k0, k0 + KT <= seen.until(k0, is_new));
       k0 = next_k0;
       is_new = next_new;
       if (t + 2 * kFewWaves < t1) {
@@ -901,7 +972,7 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
       }
       buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
     }
-    if (ld.bad) poison = u;
+    if (ld.met_bad()) poison = u;
     // the four waves' sums meet in LDS: references, row sums, outputs
     float *mine = reinterpret_cast<float *>(&tiles[wave][0][0][0]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
