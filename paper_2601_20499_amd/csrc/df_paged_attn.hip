@@ -15,7 +15,13 @@
 // through a private ring in LDS and never meets the others until the end.  Many rows are bound by the matrix core: four
 // waves of 32 rows share tiles of 64 keys.
 //
-// Sharing out.  Lengths are on the device, so the launch is, too: all workgroups add up the cost of all units (request, key
+// Sharing out.  A line of work is cut into spans (below).  Rows of the same key head read the same keys, many times more than an XCD's L2
+// holds, so the workgroups of an XCD should read the same tiles at about the same time: a workgroup of the second kernel that comes to a
+// unit t tiles after its start begins it at tile t (modulo their number), goes round, and where its span ends within the unit
+// the next workgroup does the rest of the round.  All of them start at the same tile, and a workgroup on its first unit
+// and one that is past it are the only two places that are read.  1280x720 chunk: 21 GB past the L2s without the turn, FETCH with it.
+//
+// Lengths are on the device, so the launch is, too: all workgroups add up the cost of all units (request, key
 // head, tile of rows; cost = tiles of keys + a constant), and workgroup w takes the w-th of equal spans of that line.  A
 // unit that a span's end cuts leaves partial sums in the workspace; a second kernel puts them together.
 #include <algorithm>
@@ -198,6 +204,18 @@ struct Span {
   int64_t begin, end;        // on the line
   int unit;                  // the unit that `begin` lies in, -1: there is no span for this workgroup
   int64_t unit_at;           // where that unit begins
+  int64_t all;               // length of the line
+  int count;                 // spans
+
+  // Where a span begins (of the one behind the last: the line's end).
+  __device__ __forceinline__ int64_t begin_of(int i) const { return all * i / count; }
+  // How far into its span position x of the line lies.
+  __device__ __forceinline__ int64_t into_span(int64_t x) const {
+    int i = int(x * count / all);
+    while (begin_of(i) > x) --i;
+    while (begin_of(i + 1) <= x) ++i;
+    return x - begin_of(i);
+  }
 };
 
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -240,15 +258,17 @@ __device__ __forceinline__ Span my_span(const PagedParams &p, int64_t *scratch) 
     all += s;
   }
   const int wgs = gridDim.x;
-  const int count = int(max(min(int64_t(wgs), all / kMinSpan), int64_t(all > 0)));
   Span sp;
+  sp.all = uniform(all);
+  sp.count = __builtin_amdgcn_readfirstlane(int(max(min(int64_t(wgs), all / kMinSpan), int64_t(all > 0))));
+  const int count = sp.count;
   // Workgroups are dealt to the eight XCDs in turn: with a full launch an XCD takes neighbouring spans, which read the same keys.
   sp.index = count == wgs && wgs % 8 == 0 ? int(blockIdx.x % 8) * (wgs / 8) + int(blockIdx.x / 8) : int(blockIdx.x);
   sp.begin = sp.end = sp.unit_at = 0;
   sp.unit = -1;
   if (sp.index >= count) return sp;
-  sp.begin = uniform(all * sp.index / count);
-  sp.end = uniform(all * (sp.index + 1) / count);
+  sp.begin = sp.begin_of(sp.index);
+  sp.end = sp.begin_of(sp.index + 1);
   if (mine > 0 && sp.begin >= base && sp.begin < base + mine) {
     int64_t at = base;
     walk([&](int u, int cost) {
@@ -353,7 +373,8 @@ __device__ __forceinline__ void load_group(const RowSource &src, const unsigned 
   }
 }
 
-// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles.  Uniform but for what lies in lanes.  Tiles that lie
+// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles and round again (tile t is tile t - count from the last
+// on).  Uniform but for what lies in lanes.  Tiles that lie
 // one behind the other are a run; where one begins (and every 64 tiles) seek looks up where the rows of the next 64 tiles lie, a
 // tile to a lane, so that a step has only to read a lane.
 template <int D, int KT, int GROUPS, int STEP>           // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
@@ -383,14 +404,14 @@ struct Feed {
     seek();
   }
   __device__ __forceinline__ void seek() {
-    const int hist = tl.nA + tl.nB, me = threadIdx.x & 63;
+    const int hist = tl.nA + tl.nB, me = threadIdx.x & 63, all = tl.count(), at = t >= all ? t - all : t;
     int last;                                            // tile behind the run's last
-    is_new = t >= hist;
+    is_new = at >= hist;
     if (!is_new) {
-      k0 = (t < tl.nA ? t : tl.firstB + t - tl.nA) * KT;
-      last = t < tl.nA ? tl.nA : tl.firstB + tl.nB;
+      k0 = (at < tl.nA ? at : tl.firstB + at - tl.nA) * KT;
+      last = at < tl.nA ? tl.nA : tl.firstB + tl.nB;
     } else {
-      const int i = t - hist;
+      const int i = at - hist;
       k0 = (i < tl.nC ? i : tl.firstD + i - tl.nC) * KT;
       last = i < tl.nC ? tl.nC : tl.firstD + tl.nD;
     }
@@ -819,8 +840,17 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
     const RowRange x = row_range(p, r, un.row0, ROWS);
     const Tiles<KT> tl = tiles_of<KT>(p, r, x);
     const int nt = tl.count();
-    const int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
-    const bool owns = sp.begin <= at;
+    int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
+    const bool owns = sp.begin <= at, begins = t0 == 0, ends = t1 == nt;
+    if (nt > 0) {
+      const int turn = int(sp.into_span(at) % nt);
+      t0 += turn;
+      t1 += turn;
+      if (t0 >= nt) {
+        t0 -= nt;
+        t1 -= nt;
+      }
+    }
     at += kUnitCost + nt;
     if (t0 >= t1 && !(nt == 0 && owns)) continue;
 
@@ -884,7 +914,7 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
       l += __shfl_xor(l, 32);
       if (nan) l = NAN;
       const int row = row0 + 16 * qb + (lane & 15), g = lane >> 4;
-      if (t0 == 0 && t1 == nt) {
+      if (begins && ends) {
         if (row < r.n * p.G) {
           const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -892,7 +922,7 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
           if (p.lse && g == 0) store_lse(p, r, un.h, row, rows.m[qb], l);
         }
       } else {
-        float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, t0 == 0);
+        float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, begins);
         const int in_unit = row - un.row0;
 #pragma unroll
         for (int db = 0; db < L::CH / 2; ++db) *reinterpret_cast<f32x4 *>(slot + in_unit * D + 16 * db + 4 * g) = rows.o[db][qb];
@@ -902,8 +932,8 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
         }
       }
     }
-    if (t0 == 0 && t1 < nt) note.tail_unit = u;
-    if (t0 > 0) note.head = t1 == nt ? 2 : 1;
+    if (begins && !ends) note.tail_unit = u;
+    if (!begins) note.head = ends ? 2 : 1;
     __syncthreads();                     // the poison of this piece has been read, the tiles may be loaded again
   }
   if (!p.whole && tid == 0) reinterpret_cast<Note *>(p.ws)[sp.index] = note;
