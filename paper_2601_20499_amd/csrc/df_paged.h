@@ -1,21 +1,10 @@
-// What the paged cache's translation units share: the slots of a head, and the host's checks of a df_paged_cache.
+// What the paged cache's translation units share on the host: checks of a df_paged_cache.
 #pragma once
 
 #include "df_internal.h"
+#include "df_paged_walk.h"
 
 namespace df {
-
-constexpr int kMaxLen = 1 << 30;       // bound of lengths, sinks and windows
-
-__host__ __device__ inline int clamp_int(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
-
-// Filled slots after `len` tokens: min(len, sink + win), whose sum may not fit into 32 bits.
-__host__ __device__ inline int filled_slots(int len, int sink, int win) {
-  return len < sink || len - sink < win ? len : sink + win;
-}
-
-// Slot of position j in a head with a window, and of a sink position in any.
-__host__ __device__ inline int slot_of(int j, int sink, int win) { return j < sink ? j : sink + (j - sink) % win; }
 
 inline int log2_of(int x) {
   int n = 0;

@@ -15,11 +15,12 @@
 // through a private ring in LDS and never meets the others until the end.  Many rows are bound by the matrix core: four
 // waves of 32 rows share tiles of 64 keys.
 //
-// Sharing out.  A line of work is cut into spans (below).  Rows of the same key head read the same keys, many times more than an XCD's L2
-// holds, so the workgroups of an XCD should read the same tiles at about the same time: a workgroup of the second kernel that comes to a
-// unit t tiles after its start begins it at tile t (modulo their number), goes round, and where its span ends within the unit
-// the next workgroup does the rest of the round.  All of them start at the same tile, and a workgroup on its first unit
-// and one that is past it are the only two places that are read.  1280x720 chunk: 21 GB past the L2s without the turn, FETCH with it.
+// Sharing out.  Rows of the same key head read the same keys.  Where these are more than an XCD's L2 holds, its workgroups should read the same
+// tiles at about the same time: a workgroup of the second kernel that comes to a unit t tiles after its start begins it at tile t (modulo
+// their number) and goes round, and where its span ends within the unit the next workgroup does the rest of the round.  All of them start
+// at the same tile, so at any time two places are read, by the workgroups on their first unit and by those past it.  1280x720 chunk: 21 GB
+// fetched past the L2s without this, 2.8 GB with it, and 2990 -> 2620 us.  Keys that fit are better read from the first to the last
+// (fewer runs of tiles: 390-token frames 85 us, 89 with turned rounds).
 //
 // Lengths are on the device, so the launch is, too: all workgroups add up the cost of all units (request, key
 // head, tile of rows; cost = tiles of keys + a constant), and workgroup w takes the w-th of equal spans of that line.  A
@@ -74,8 +75,10 @@ struct PagedParams {
   int64_t cap_stride;
   unsigned kc_tok;           // bytes
   int B, Hkv, Hq, G;
+  Rules rules;
+  Divider by_tiles, by_heads;
   int page_log2, n_pages, max_pages;
-  int total, max_new, block;
+  int total, max_new;
   int row_tiles;             // tiles of rows of max_new tokens
   int units;                 // B * Hkv * row_tiles
   float c;                   // scale * log2(e)
@@ -85,163 +88,60 @@ struct PagedParams {
 };
 
 constexpr int kThreads = 256;
-constexpr int kUnitCost = 4;           // cost of a unit besides its tiles, in tiles
-constexpr int kSnap = 3;               // no piece of a cut unit has fewer tiles ...
-constexpr int kMinSpan = 8;            // ... than fit into the shortest span; units of up to kMinSpan tiles are not cut
-static_assert(2 * kSnap < kMinSpan, "a span inside a unit is a piece");
-
-// A request as one key head sees it.
-struct Request {
-  int n, q0;                 // new tokens and the first one's row
-  int L, s, w, held;         // tokens in the cache, sink, window, filled slots
-  bool bad;                  // more slots than the table has entries for
-};
-
 __device__ __forceinline__ Request request_of(const PagedParams &p, int b, int h) {
-  Request r;
-  const int c0 = clamp_int(p.cu[b], 0, p.total), c1 = clamp_int(p.cu[b + 1], c0, p.total);
   const int64_t cap = b * p.cap_stride + h;
-  r.q0 = c0;
-  r.n = min(c1 - c0, p.max_new);
-  r.L = clamp_int(p.len[b], 0, kMaxLen);
-  r.s = clamp_int(p.sink[cap], 0, kMaxLen);
-  r.w = clamp_int(p.win[cap], 0, kMaxLen);
-  r.held = filled_slots(r.L, r.s, r.w);
-  const int64_t room = int64_t(p.max_pages) << p.page_log2;
-  r.bad = r.held > room;
-  if (r.bad) r.held = int(room);
-  return r;
-}
-
-// Slots that a causal block beginning at new token `first` sees: [0, a1) and [b0, b1).  Behind the sink they are a ring; what the
-// block does not see of it are the `first` oldest tokens (or, before the ring is full, those older than the window).
-struct Visible { int a1, b0, b1; };
-__device__ __forceinline__ Visible visible_slots(const Request &r, int first) {
-  Visible v;
-  const int sink = min(r.held, r.s), turn = r.L - r.s;
-  if (first >= r.w || turn <= 0) {
-    v.a1 = v.b0 = v.b1 = sink;
-  } else if (turn <= r.w) {
-    const int lo = r.L + first - r.w;
-    v.a1 = lo <= r.s ? r.held : sink;
-    v.b0 = lo <= r.s ? r.held : min(lo, r.held);
-    v.b1 = r.held;
-  } else if (first == 0) {
-    v.a1 = v.b0 = v.b1 = r.held;
-  } else {
-    const int at = turn % r.w;
-    const bool wraps = at > r.w - first;
-    v.a1 = min(r.held, wraps ? r.s : r.s + at);
-    v.b0 = min(r.held, wraps ? r.s + (at - (r.w - first)) : r.s + at + first);
-    v.b1 = min(r.held, wraps ? r.s + at : r.s + r.w);
-  }
-  return v;
-}
-
-// The key tiles of one unit: slots first, new tokens behind them, each in up to two runs of tiles.
-template <int KT>
-struct Tiles {
-  int nA, nB, nC, nD;        // tiles of the four runs
-  int firstB, firstD;        // first tile of the second runs (the first ones begin at 0)
-  __device__ __forceinline__ int count() const { return nA + nB + nC + nD; }
-};
-
-struct RowRange {
-  int first0, first1;        // first tokens of the first and the last row's causal blocks
-  int end0, end1;            // and their ends
-};
-__device__ __forceinline__ RowRange row_range(const PagedParams &p, const Request &r, int row0, int rows) {
-  RowRange x;
-  const int block = min(p.block, max(r.n, 1));
-  const int i0 = row0 / p.G, i1 = min(r.n - 1, (row0 + rows - 1) / p.G);
-  x.first0 = i0 / block * block;
-  x.first1 = i1 / block * block;
-  x.end0 = min(x.first0 + block, r.n);
-  x.end1 = min(x.first1 + block, r.n);
-  return x;
-}
-
-template <int KT>
-__device__ __forceinline__ Tiles<KT> tiles_of(const PagedParams &p, const Request &r, const RowRange &x) {
-  Tiles<KT> t;
-  const Visible v = visible_slots(r, x.first0);
-  t.nA = (v.a1 + KT - 1) / KT;
-  t.firstB = max(v.b0 / KT, t.nA);
-  t.nB = v.b1 > v.b0 ? max(0, (v.b1 + KT - 1) / KT - t.firstB) : 0;
-  t.nC = t.nD = t.firstD = 0;
-  if (p.k_cur) {
-    const int c1 = clamp_int(r.s - r.L, 0, x.end1), d0 = max(0, x.first0 - r.w);
-    t.nC = (c1 + KT - 1) / KT;
-    t.firstD = max(d0 / KT, t.nC);
-    t.nD = max(0, (x.end1 + KT - 1) / KT - t.firstD);
-  }
-  return t;
-}
-
-// Unit u of the line: requests outermost, then key heads, then tiles of rows (neighbours read the same keys).
-struct Unit { int b, h, row0; };
-__device__ __forceinline__ Unit unit_of(const PagedParams &p, int u, int rows) {
-  const int e = u / p.row_tiles;
-  return Unit{e / p.Hkv, e % p.Hkv, (u - e * p.row_tiles) * rows};
-}
-
-// Cost of a unit on the line, 0 if it has no rows.
-template <int KT, int ROWS>
-__device__ __forceinline__ int unit_cost(const PagedParams &p, const Request &r, int row0) {
-  if (row0 >= r.n * p.G) return 0;
-  return kUnitCost + tiles_of<KT>(p, r, row_range(p, r, row0, ROWS)).count();
-}
-
-// Tile at which position x of a unit's part of the line (its first kUnitCost positions are no tiles) cuts its T tiles.
-__device__ __forceinline__ int cut_at(int64_t x, int T) {
-  if (T <= kMinSpan) return x <= 0 ? 0 : T;
-  const int64_t t = x - kUnitCost;
-  return t < kSnap ? 0 : t > T - kSnap ? T : int(t);
+  return make_request(p.cu[b], p.cu[b + 1], p.len[b], p.sink[cap], p.win[cap], p.total, p.max_new, int64_t(p.max_pages) << p.page_log2);
 }
 
 struct Span {
+  Line line;
   int index;                 // number of the span
   int64_t begin, end;        // on the line
   int unit;                  // the unit that `begin` lies in, -1: there is no span for this workgroup
   int64_t unit_at;           // where that unit begins
-  int64_t all;               // length of the line
-  int count;                 // spans
-
-  // Where a span begins (of the one behind the last: the line's end).
-  __device__ __forceinline__ int64_t begin_of(int i) const { return all * i / count; }
-  // How far into its span position x of the line lies.
-  __device__ __forceinline__ int64_t into_span(int64_t x) const {
-    int i = int(x * count / all);
-    while (begin_of(i) > x) --i;
-    while (begin_of(i + 1) <= x) ++i;
-    return x - begin_of(i);
-  }
 };
 
+__device__ __forceinline__ int64_t least64(int64_t a, int64_t b) { return a < b ? a : b; }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
   return int64_t(unsigned(__builtin_amdgcn_readfirstlane(int(x)))) | int64_t(__builtin_amdgcn_readfirstlane(int(x >> 32))) << 32;
 }
 
-// This workgroup's span.  Every workgroup adds up all units; `scratch` is LDS, at least (kThreads / 64 + 2) 8-byte words.
+// This workgroup's span.  Every workgroup adds up all units; `lds` is kStaged * 16 bytes of LDS and `scratch` kThreads / 64 + 2 words.  What a unit costs depends on
+// four numbers of its (request, key head), which are brought to LDS first, all in one trip to memory: read unit by unit, a thousand units took
+// 10 us, and 2500 25.
+constexpr int kStaged = 2048;
+struct Entry { int n, L, s, w; };
 template <int KT, int ROWS>
-__device__ __forceinline__ Span my_span(const PagedParams &p, int64_t *scratch) {
+__device__ __forceinline__ Span my_span(const PagedParams &p, Entry *lds, int64_t *scratch) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (p.units + kThreads - 1) / kThreads;
-  const int u0 = min(tid * per, p.units), u1 = min(u0 + per, p.units);
-  auto walk = [&](auto &&each) {
-    int known = -1;
-    Request r{};
-    for (int u = u0; u < u1; ++u) {
-      const int e = u / p.row_tiles;
-      if (e != known) {
-        known = e;
-        r = request_of(p, e / p.Hkv, e % p.Hkv);
-      }
-      each(u, unit_cost<KT, ROWS>(p, r, (u - e * p.row_tiles) * ROWS));
-    }
+  const int entries = p.B * p.Hkv;
+  const bool staged = entries <= kStaged;
+  auto load = [&](int e) {
+    const int b = p.by_heads.of(e);
+    const Request r = request_of(p, b, e - b * p.Hkv);
+    return Entry{r.n, r.L, r.s, r.w};
   };
+  if (staged) {
+#pragma unroll 4
+    for (int e = tid; e < entries; e += kThreads) lds[e] = load(e);
+    __syncthreads();
+  }
+  auto cost = [&](int u) {
+    if (u >= p.units) return 0;
+    const int e = p.by_tiles.of(u), row0 = (u - e * p.row_tiles) * ROWS;
+    const Entry x = staged ? lds[e] : load(e);
+    if (row0 >= x.n * p.G) return 0;
+    Request r;
+    r.n = x.n;
+    r.L = x.L;
+    r.s = x.s;
+    r.w = x.w;
+    r.held = int(least64(filled_slots(x.L, x.s, x.w), int64_t(p.max_pages) << p.page_log2));
+    return kUnitCost + tiles_of<KT>(r, row_range(r, p.rules, row0, ROWS), p.rules.keys).count();
+  };
+  const int per = (p.units + kThreads - 1) / kThreads;
   int64_t mine = 0;
-  walk([&](int, int cost) { mine += cost; });
+  for (int i = 0; i < per; ++i) mine += cost(tid * per + i);
   int64_t incl = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -259,29 +159,43 @@ __device__ __forceinline__ Span my_span(const PagedParams &p, int64_t *scratch) 
   }
   const int wgs = gridDim.x;
   Span sp;
-  sp.all = uniform(all);
-  sp.count = __builtin_amdgcn_readfirstlane(int(max(min(int64_t(wgs), all / kMinSpan), int64_t(all > 0))));
-  const int count = sp.count;
+  sp.line.all = uniform(all);
+  sp.line.count = __builtin_amdgcn_readfirstlane(span_count(all, wgs));
+  const int count = sp.line.count;
   // Workgroups are dealt to the eight XCDs in turn: with a full launch an XCD takes neighbouring spans, which read the same keys.
   sp.index = count == wgs && wgs % 8 == 0 ? int(blockIdx.x % 8) * (wgs / 8) + int(blockIdx.x / 8) : int(blockIdx.x);
   sp.begin = sp.end = sp.unit_at = 0;
   sp.unit = -1;
   if (sp.index >= count) return sp;
-  sp.begin = sp.begin_of(sp.index);
-  sp.end = sp.begin_of(sp.index + 1);
+  sp.begin = sp.line.begin_of(sp.index);
+  sp.end = sp.line.begin_of(sp.index + 1);
+  // whose units hold it ...
   if (mine > 0 && sp.begin >= base && sp.begin < base + mine) {
-    int64_t at = base;
-    walk([&](int u, int cost) {
-      if (sp.begin >= at && sp.begin < at + cost) {
-        scratch[kThreads / 64] = u;
-        scratch[kThreads / 64 + 1] = at;
-      }
-      at += cost;
-    });
+    scratch[kThreads / 64] = tid;
+    scratch[kThreads / 64 + 1] = base;
   }
   __syncthreads();
-  sp.unit = int(uniform(scratch[kThreads / 64]));
-  sp.unit_at = uniform(scratch[kThreads / 64 + 1]);
+  // ... and which of them, a unit to a lane
+  const int u0 = __builtin_amdgcn_readfirstlane(int(scratch[kThreads / 64])) * per;
+  int64_t at = uniform(scratch[kThreads / 64 + 1]);
+  for (int i = 0; i < per; i += 64) {
+    const int c = i + lane < per ? cost(u0 + i + lane) : 0;
+    int upto = c;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(upto, d);
+      if (lane >= d) upto += y;
+    }
+    const uint64_t in = __builtin_amdgcn_ballot_w64(c > 0 && sp.begin >= at + upto - c && sp.begin < at + upto);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      sp.unit = u0 + i + l;
+      sp.unit_at = at + __builtin_amdgcn_readlane(upto - c, l);
+      break;
+    }
+    at += __builtin_amdgcn_readlane(upto, 63);
+  }
+  __syncthreads();                       // the numbers in LDS make room for tiles
   return sp;
 }
 
@@ -323,6 +237,18 @@ struct Layout {
 };
 // Key (of 32) that operand row m of block u (of two) holds; the block's scores 4 g + v, u = 0, 1 are then keys 8 g + 4 u + v.
 __device__ __forceinline__ int key_of_operand_row(int m, int u) { return 8 * (m >> 2) + 4 * u + (m & 3); }
+
+// The lane, as a value that the compiler does not know from before: what is derived from it is worked out where it is used.  Left to itself the
+// compiler works everything out once, keeps more than there are registers, and what it reloads from scratch memory waits for all
+// loads on their way, the next tile's among them.
+__device__ __forceinline__ int lane_here() {
+  int x = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Workgroup barrier that waits for this wave's LDS traffic only: stores of finished rows stay on their way (with a wait for them a piece took 3 us longer).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 __device__ __forceinline__ unsigned lds_address(const void *ptr) { return unsigned(reinterpret_cast<uintptr_t>(ptr)); }
 
@@ -373,115 +299,135 @@ __device__ __forceinline__ void load_group(const RowSource &src, const unsigned 
   }
 }
 
-// Brings the tiles of a unit to LDS, every STEP-th of them, in the order of Tiles and round again (tile t is tile t - count from the last
-// on).  Uniform but for what lies in lanes.  Tiles that lie
-// one behind the other are a run; where one begins (and every 64 tiles) seek looks up where the rows of the next 64 tiles lie, a
-// tile to a lane, so that a step has only to read a lane.
+// Brings the tiles of a piece to LDS, every STEP-th of them.  Everything about the next 64 of them is worked out at once, a tile to a lane (look_ahead): where its
+// rows lie, and what the wave's rows see of it.  A step then reads a lane and shifts some masks.
 template <int D, int KT, int GROUPS, int STEP>           // GROUPS of 16 rows that the wave brings of a tile, from its group `grp0` on
 struct Feed {
   using L = Layout<D>;
   const PagedParams &p;
   const Request &r;
   const Tiles<KT> &tl;
-  const int grp0;
+  const RangeKeys &seen;
+  const bool live;           // the wave has rows
+  const int grp0, end;       // tile behind the piece's last
   const_int *pages;          // the head's row of the block table
   const int64_t cur;         // byte offset of the request's first new token of the head
-  int t;                     // the tile that is brought next,
-  int k0;                    // its first key,
-  int left, whole;           // tiles and whole tiles from it on in its run, itself among them,
-  int lane;                  // and where its rows are noted
-  bool is_new;
-  const char *kb, *vb;       // row 0
-  unsigned stride;           // bytes between rows
-  int limit;                 // keys that are there
-  unsigned slots[GROUPS];    // lane i: the first row of tile t + STEP i's group
-  unsigned ko[GROUPS][L::LPG], vo[GROUPS][L::LPG];       // the lane's 16 bytes of every load, from the group's first row on
-  bool bad;                  // a page was no page of the pool
+  int t, lane;               // the tile that is brought next, and its lane
+  unsigned slots[GROUPS];    // per lane: first row of the tile's group, among the head's pages or the request's new tokens
+  int keys;                  // per lane: the tile's first key
+  uint64_t there, fresh, whole, seen1, seen2;            // tiles that exist, of new tokens, with all rows, and what is seen of them (two bits)
+  bool bad;                  // per lane: a page was no page of the pool
 
-  __device__ __forceinline__ Feed(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, int b, int h, int grp0_, int t_)
-      : p(p_), r(r_), tl(tl_), grp0(grp0_), pages(p_.table + (int64_t(b) * p_.Hkv + h) * p_.max_pages),
-        cur(int64_t(r_.q0) * p_.kc_tok + h * p_.kc_head), t(t_), bad(r_.bad) {
-    seek();
+  __device__ __forceinline__ Feed(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, const RangeKeys &seen_, bool live_, int b, int h, int grp0_,
+                                  int begin, int end_)
+      : p(p_), r(r_), tl(tl_), seen(seen_), live(live_), grp0(grp0_), end(end_), pages(p_.table + (int64_t(b) * p_.Hkv + h) * p_.max_pages),
+        cur(int64_t(r_.q0) * p_.kc_tok + h * p_.kc_head), t(begin), bad(r_.bad) {
+    look_ahead();
   }
-  __device__ __forceinline__ void seek() {
-    const int hist = tl.nA + tl.nB, me = threadIdx.x & 63, all = tl.count(), at = t >= all ? t - all : t;
-    int last;                                            // tile behind the run's last
-    is_new = at >= hist;
-    if (!is_new) {
-      k0 = (at < tl.nA ? at : tl.firstB + at - tl.nA) * KT;
-      last = at < tl.nA ? tl.nA : tl.firstB + tl.nB;
-    } else {
-      const int i = at - hist;
-      k0 = (i < tl.nC ? i : tl.firstD + i - tl.nC) * KT;
-      last = i < tl.nC ? tl.nC : tl.firstD + tl.nD;
-    }
-    limit = is_new ? r.n : r.held;
-    left = last - k0 / KT;
-    whole = min(last, limit / KT) - k0 / KT;
-    lane = 0;
-    stride = is_new ? p.kc_tok : unsigned(L::ROWB);
-    kb = is_new ? p.k_cur + cur : p.k_pages;
-    vb = is_new ? p.v_cur + cur : p.v_pages;
+  __device__ __forceinline__ void look_ahead() {
+    const int mine = t + STEP * lane_here();
+    const Place x = place_of(r, tl, mine);
+    const bool is = mine < end;
+    const int what = live ? int(seen_of(x, KT, seen)) : int(kNoneSeen);
+    keys = x.k0;
+    there = __builtin_amdgcn_ballot_w64(is);
+    fresh = __builtin_amdgcn_ballot_w64(x.is_new);
+    whole = __builtin_amdgcn_ballot_w64(is && x.k0 + KT <= x.limit);
+    seen1 = __builtin_amdgcn_ballot_w64(what & 1);
+    seen2 = __builtin_amdgcn_ballot_w64(what & 2);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int row = k0 + me * (STEP * KT) + 16 * (grp0 + g);
-      slots[g] = is_new ? row : 0;
-      if (!is_new && me * STEP < left && row < limit) {
+      const int row = x.k0 + 16 * (grp0 + g);
+      slots[g] = x.is_new ? row : 0;
+      if (is && !x.is_new && row < x.limit) {
         const int page = pages[row >> p.page_log2];
         const bool is_page = unsigned(page) < unsigned(p.n_pages);
         bad |= !is_page;
         slots[g] = is_page ? (unsigned(page) << p.page_log2) + unsigned(row & ((1 << p.page_log2) - 1)) : 0;
       }
+    }
+    lane = 0;
+  }
+  __device__ __forceinline__ bool next_is_new() const { return fresh >> lane & 1; }
+  __device__ __forceinline__ const char *k_base(bool is_new) const { return is_new ? p.k_cur + cur : p.k_pages; }
+  __device__ __forceinline__ const char *v_base(bool is_new) const { return is_new ? p.v_cur + cur : p.v_pages; }
+  __device__ __forceinline__ unsigned stride(bool is_new) const { return is_new ? p.kc_tok : unsigned(L::ROWB); }
+  // Where the lane's 16 bytes of every load of group g lie behind the group's first row, of rows `stride` bytes apart.
+  __device__ __forceinline__ void aim(int g, unsigned stride, unsigned (&ko)[L::LPG], unsigned (&vo)[L::LPG]) const {
+    const int me = lane_here();
 #pragma unroll
-      for (int i = 0; i < L::LPG; ++i) {
-        const int in_group = i * L::RPL + me / L::CH, place = (grp0 + g) * 16 + in_group;
-        ko[g][i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::k_turn(place));
-        vo[g][i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::v_turn(place));
-      }
+    for (int i = 0; i < L::LPG; ++i) {
+      const int in_group = i * L::RPL + me / L::CH, place = (grp0 + g) * 16 + in_group;
+      ko[i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::k_turn(place));
+      vo[i] = unsigned(in_group) * stride + 16u * unsigned((me % L::CH) ^ L::v_turn(place));
     }
   }
-  // The tile's rows to LDS: K rows of the tile at `k_to`, V rows at `v_to`; then on by STEP tiles, if there is one before tile `end`.
-  __device__ __forceinline__ void bring(unsigned k_to, unsigned v_to, int end) {
+  // A tile that is under way.
+  struct Coming {
+    int k0, seen;
+    bool is_new;
+  };
+  __device__ __forceinline__ Coming coming(int at) const {
+    return Coming{__builtin_amdgcn_readlane(keys, at), int(seen1 >> at & 1) | int(seen2 >> at & 1) << 1, bool(fresh >> at & 1)};
+  }
+  // The next tile's rows to LDS, K rows of the tile at `k_to` and V rows at `v_to`; then on to the one behind it.
+  __device__ __forceinline__ Coming bring(unsigned k_to, unsigned v_to) {
+    const Coming c = coming(lane);
+    const char *kb = k_base(c.is_new), *vb = v_base(c.is_new);
+    const unsigned apart = stride(c.is_new);
+    const int limit = pick(c.is_new, r.n, r.held);
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int rows = clamp_int(limit - (k0 + 16 * (grp0 + g)), 0, 16);
-      const uint64_t at = uint64_t(unsigned(__builtin_amdgcn_readlane(int(slots[g]), lane))) * stride;
-      const unsigned bytes = rows > 0 ? unsigned(rows - 1) * stride + L::ROWB : 0;
-      load_group<D>(RowSource{kb + at, vb + at, bytes}, ko[g], vo[g], k_to + (grp0 + g) * 16 * L::ROWB, v_to + (grp0 + g) * 16 * L::ROWB);
+      const int rows = clamp_int(limit - (c.k0 + 16 * (grp0 + g)), 0, 16);
+      const uint64_t at = uint64_t(unsigned(__builtin_amdgcn_readlane(int(slots[g]), lane))) * apart;
+      const unsigned bytes = rows > 0 ? unsigned(rows - 1) * apart + L::ROWB : 0;
+      unsigned ko[L::LPG], vo[L::LPG];
+      aim(g, apart, ko, vo);
+      load_group<D>(RowSource{kb + at, vb + at, bytes}, ko, vo, k_to + (grp0 + g) * 16 * L::ROWB, v_to + (grp0 + g) * 16 * L::ROWB);
     }
-    on(1, end);
+    on(1);
+    return c;
   }
-  __device__ __forceinline__ void on(int steps, int end) {
+  __device__ __forceinline__ void on(int steps) {
     t += STEP * steps;
-    k0 += STEP * steps * KT;
-    left -= STEP * steps;
-    whole -= STEP * steps;
     lane += steps;
-    if (__builtin_expect(t < end && (left <= 0 || lane >= 64), 0)) seek();
+    if (__builtin_expect(lane == 64 && t < end, 0)) look_ahead();
+  }
+  // How many steps can be taken, from the tile under way on, in which the tile is one that all rows see and the one behind it, of the kind of the
+  // next, has all of its rows.
+  __device__ __forceinline__ int steps(const Coming &now) const {
+    if (lane == 64) return 0;
+    const uint64_t all = ~(seen1 | seen2) << 1, here = uint64_t(1) << lane;
+    uint64_t x = (now.seen == kAllSeen ? all | here : all & ~here) & whole & (next_is_new() ? fresh : ~fresh);
+    x = ~(x >> lane);
+    return x ? __builtin_ctzll(x) : 64;
   }
   // Whether a page of the wave's was none, in any lane.
   __device__ __forceinline__ bool met_bad() const { return __builtin_amdgcn_ballot_w64(bad) != 0; }
 };
 
-// Keys that every row of a range sees, of the cache and of the new tokens: [0, a) and [b, c) (uniform).
-struct Free { int a, b, c; };
-struct FreeKeys {
-  Free hist, fresh;
-  // Key behind the last of the keys from k0 on that are seen without a gap, k0 itself or less if it is not.
-  __device__ __forceinline__ int until(int k0, bool is_new) const {
-    const int a = is_new ? fresh.a : hist.a, b = is_new ? fresh.b : hist.b, c = is_new ? fresh.c : hist.c;
-    return k0 < a ? a : k0 >= b ? c : k0;
+// ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
+
+// What masks need to know of a wave's rows, worked out once a piece, in LDS.
+template <int ROWS>
+struct RowNotes {
+  int first[ROWS];           // first token of the row's causal block
+  int ring;                  // slots of the ring in front of its oldest token
+  __device__ __forceinline__ void fill(const PagedParams &p, const Request &r, int row0) {
+    const int lane = threadIdx.x & 63;
+    if (lane < ROWS) first[lane] = p.rules.first_of(min(row0 + lane, r.n * p.G - 1));
+    if (lane == 0) ring = ring_start(r);
+  }
+  __device__ __forceinline__ Sight sight(const PagedParams &p, const Request &r, int qb, bool is_new) const {
+    return Sight::behind(r, p.rules, first[16 * qb + (lane_here() & 15)], is_new);
   }
 };
-__device__ __forceinline__ FreeKeys free_keys(const Request &r, const RowRange &x) {
-  FreeKeys f;
-  const Visible v = visible_slots(r, x.first1);
-  f.hist = Free{v.a1, v.b0, v.b1};
-  f.fresh = Free{clamp_int(r.s - r.L, 0, x.end0), max(0, x.first1 - r.w), x.end0};
-  return f;
-}
-
-// ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
+// The products of a tile of 64 keys and 32 rows, each as one asm statement (df_paged_tiles.inc; operands on their way from LDS as in the loop over
+// tiles): S^T from the lane's first K operand on, O^T from its first V^T operand on.
+template <class T, int D>
+__device__ __forceinline__ void scores_of(unsigned first, const s16x8 (&q)[D / 32][2], f32x4 (&s)[4][2]);
+template <class T, int D>
+__device__ __forceinline__ void values_of(unsigned first, const s16x8 (&w)[2][2], f32x4 (&o)[D / 16][2]);
 
 template <class T, int D, int KB, int QB>      // KB blocks of 16 keys, QB blocks of 16 rows
 struct Rows {
@@ -510,7 +456,7 @@ struct Rows {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int row = min(row0 + 16 * qb + (lane & 15), r.n * p.G - 1);
-      const int i = row / p.G, head = h * p.G + row - i * p.G;
+      const int i = p.rules.G.of(row), head = h * p.G + row - i * p.G;
       const char *src = p.q + int64_t(r.q0 + i) * p.q_tok + head * p.q_head + 16 * g;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) q[ks][qb] = *reinterpret_cast<const s16x8 *>(src + 64 * ks);
@@ -528,7 +474,7 @@ struct Rows {
   // Where the lane reads K of a tile at `k`: chunk 4 ks + lane / 16 of its operand row, for ks = 0.  (Tiles begin at multiples of 1 KB, so
   // ks turns bits of the address.)
   __device__ __forceinline__ static unsigned k_first(unsigned k) {
-    const int lane = threadIdx.x & 63, row = key_of_operand_row(lane & 15, 0);
+    const int lane = lane_here(), row = key_of_operand_row(lane & 15, 0);
     return k + unsigned(row * Layout<D>::ROWB + 16 * ((lane >> 4) ^ Layout<D>::k_turn(row)));
   }
 
@@ -537,6 +483,7 @@ struct Rows {
   __device__ __forceinline__ void scores(unsigned k, f32x4 (&s)[KB][QB]) const {
     using L = Layout<D>;
     const unsigned first = k_first(k);
+    if constexpr (KB == 4 && QB == 2) return scores_of<T, D>(first, q, s);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const unsigned at = first ^ unsigned(64 * ks);
@@ -559,42 +506,21 @@ struct Rows {
     __builtin_amdgcn_sched_group_barrier(0x8, A * QB, 0);
   }
 
-  // What the lane's rows see of a tile's keys.
-  struct Sight {
-    int lim[QB], end[QB];    // lowest position, and key behind the last one
-    int at;                  // slots of the ring in front of its oldest token
-    bool is_new, wrapped;
-    __device__ __forceinline__ Sight(const PagedParams &p, const Request &r, int row0, bool is_new_) : is_new(is_new_) {
-      const int lane = threadIdx.x & 63, block = min(p.block, max(r.n, 1)), turn = max(r.L - r.s, 0);
-      wrapped = turn > r.w;
-      at = wrapped && r.w > 0 ? turn % r.w : 0;
+  // Scores of keys that a row does not see, and of those before `from`, become minus infinity.  (Without a branch: with one per key, and all
+  // scores moved around each, a tile of it took 10 us.)
+  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, int k0, bool is_new, int from, f32x4 (&s)[KB][QB]) {
+    const int g = lane_here() >> 4;
+    const Order order = Order::of(r, is_new, int(scalar(unsigned(notes.ring))));
+    Sight sight[QB];
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        const int row = min(row0 + 16 * qb + (lane & 15), r.n * p.G - 1), first = row / p.G / block * block;
-        lim[qb] = (is_new ? 0 : r.L) + first - r.w;
-        end[qb] = is_new ? min(first + block, r.n) : r.held;
-      }
-    }
-    // Position of a key, the largest one where windows do not matter.
-    __device__ __forceinline__ int position(const Request &r, int key) const {
-      if (is_new) return key < r.s - r.L ? INT32_MAX : key;
-      const int k = key - r.s;
-      return k < 0 ? INT32_MAX : wrapped ? r.L - at + k - (k < at ? 0 : r.w) : key;
-    }
-    __device__ __forceinline__ bool sees(int qb, int key, int pos) const { return key < end[qb] && pos >= lim[qb]; }
-  };
-
-  // Scores of keys that a row does not see, and of those before `from`, become minus infinity.
-  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, int row0, int k0, bool is_new, int from, f32x4 (&s)[KB][QB]) {
-    const int g = (threadIdx.x & 63) >> 4;
-    const Sight sight(p, r, row0, is_new);
+    for (int qb = 0; qb < QB; ++qb) sight[qb] = notes.sight(p, r, qb, is_new);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v, pos = sight.position(r, key);
+        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v, pos = order.position(key);
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = key >= from && sight.sees(qb, key, pos) ? s[kb][qb][v] : -INFINITY;
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = ((key >= from) & sight[qb].sees(key, pos)) ? s[kb][qb][v] : -INFINITY;
       }
   }
 
@@ -643,17 +569,20 @@ struct Rows {
     all_set = !__builtin_amdgcn_ballot_w64(none);
   }
 
-  // One tile, or what of it begins at key `from`.  The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
+  // One tile, or what of it begins at key `from`; `seen` says whether all rows see all of its keys (kAllSeen), all that are there (the rows behind the last
+  // key are zeros), or not.  The reference m of a row is the largest score of the tiles up to some tile, not of all: a weight may pass one.  Only where a
   // lane's weights add up to more than 2^15 (fp16 holds weights to 2^16, and sums and outputs stay far from the largest number
   // in 32 bits), and where a row has no reference yet, the wave looks for the maximum, brings what it has to the new reference
   // and weighs the tile again.  That leaves the common tile without a maximum, a comparison per score or a product of the outputs.
-  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, int row0, unsigned k, unsigned v, int k0, bool is_new, int from, bool all_seen) {
+  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, unsigned k, unsigned v, int k0, bool is_new, int from, int seen) {
     f32x4 s[KB][QB];
     s16x8 w[KB / 2][QB];
     float sum[QB];
     scores(k, s);
-    if (__builtin_expect(!all_seen, 0)) hide(p, r, row0, k0, is_new, from, s);
-    Values x = begin_values(v);
+    if (__builtin_expect(seen != kAllSeen, 0)) hide(p, r, notes, k0, is_new, from, s);
+    constexpr bool kAsm = KB == 4 && QB == 2;
+    Values x;
+    if constexpr (!kAsm) x = begin_values(v);
     bool over = false;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -667,13 +596,15 @@ struct Rows {
     }
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
-    if (__builtin_expect(!all_seen && odd_values(v), 0)) odd_products(p, r, row0, v, k0, is_new, w); else values(x, w);
+    if (__builtin_expect(seen == kSomeHidden && odd_values(v), 0)) odd_products(p, r, notes, v, k0, is_new, w);
+    else if constexpr (kAsm) values_of<T, D>(v_first(v), w, o);
+    else values(x, w);
   }
 
   // Where the lane reads V^T of a tile at `v`: columns 16 db + lane % 16 of keys 8 g .. 8 g + 3 and, four rows on, the next four.
   __device__ __forceinline__ static unsigned v_first(unsigned v) {
     using L = Layout<D>;
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, row = 8 * g + (j >> 2);
+    const int lane = lane_here(), g = lane >> 4, j = lane & 15, row = 8 * g + (j >> 2);
     return v + unsigned(row * L::ROWB + 16 * L::v_turn(row) + 8 * (j & 3));
   }
   __device__ __forceinline__ static s16x8 v_operand(unsigned first, int ts, int db) {
@@ -722,7 +653,7 @@ struct Rows {
     for (int k = 0; k < 8; ++k) most = most > top[k] ? most : top[k];
     return __builtin_amdgcn_ballot_w64(most >= T::kExponent) != 0;
   }
-  __device__ __forceinline__ void odd_products(const PagedParams &p, const Request &r, int row0, unsigned v, int k0, bool is_new, const s16x8 (&w)[KB / 2][QB]) {
+  __device__ __forceinline__ void odd_products(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, unsigned v, int k0, bool is_new, const s16x8 (&w)[KB / 2][QB]) {
     using L = Layout<D>;
     const unsigned first = v_first(v);
 #pragma unroll
@@ -733,11 +664,14 @@ struct Rows {
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) o[i % DB][qb] = T::mfma(a, w[i / DB][qb], o[i % DB][qb]);
     }
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const Sight sight(p, r, row0, is_new);
+    const int g = lane_here() >> 4;
+    const Order order = Order::of(r, is_new, int(scalar(unsigned(notes.ring))));
+    Sight sight[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) sight[qb] = notes.sight(p, r, qb, is_new);
 #pragma unroll 1
     for (int key = 0; key < 16 * KB; ++key) {
-      const int pos = sight.position(r, k0 + key);
+      const int pos = order.position(k0 + key);
       const unsigned row = v + unsigned(key * L::ROWB);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
@@ -748,7 +682,7 @@ struct Rows {
           const bool odd = (u16(x[i]) & T::kExponent) == T::kExponent;
           const float f = odd ? ((u16(x[i]) & ~(T::kExponent | 0x8000u)) ? NAN : (u16(x[i]) & 0x8000u) ? -INFINITY : INFINITY) : 0.f;
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) o[db][qb][i] += sight.sees(qb, k0 + key, pos) ? f : 0.f;
+          for (int qb = 0; qb < QB; ++qb) o[db][qb][i] += sight[qb].sees(k0 + key, pos) ? f : 0.f;
         }
       }
     }
@@ -757,7 +691,7 @@ struct Rows {
 
 template <class T>
 __device__ __forceinline__ void store_row4(const PagedParams &p, const Request &r, int h, int row, int col, f32x4 x) {
-  const int i = row / p.G, head = h * p.G + row - i * p.G;
+  const int i = p.rules.G.of(row), head = h * p.G + row - i * p.G;
   char *dst = p.out + int64_t(r.q0 + i) * p.o_tok + head * p.o_head + 2 * col;
   uint2 y;
   y.x = T::pack(x[0], x[1]);
@@ -766,7 +700,7 @@ __device__ __forceinline__ void store_row4(const PagedParams &p, const Request &
 }
 // m and l of a finished row: l = 0 where the row sees nothing.
 __device__ __forceinline__ void store_lse(const PagedParams &p, const Request &r, int h, int row, float m, float l) {
-  const int i = row / p.G, head = h * p.G + row - i * p.G;
+  const int i = p.rules.G.of(row), head = h * p.G + row - i * p.G;
   const float log2_sum = m * p.c + __builtin_amdgcn_logf(l);
   p.lse[int64_t(head) * p.total + r.q0 + i] = l == 0.f ? -INFINITY : log2_sum * p.ln_unit;
 }
@@ -774,6 +708,7 @@ __device__ __forceinline__ void store_lse(const PagedParams &p, const Request &r
 // ---- many rows: four waves of 32 share tiles of 64 keys ---------------------------------------------------------------------------
 
 constexpr int kManyRows = 128, kManyKeys = 64;
+constexpr int kL2 = 4 << 20;           // bytes of an XCD's L2
 
 // What the loop over whole tiles that all rows of the wave see needs besides the queries.
 template <int D>
@@ -798,19 +733,16 @@ struct SeenTiles {
   }
   template <class F>
   __device__ __forceinline__ void rows_of(const F &f) {
-    const uint64_t ka = reinterpret_cast<uint64_t>(f.kb), va = reinterpret_cast<uint64_t>(f.vb);
+    const bool is_new = f.next_is_new();
+    const uint64_t ka = reinterpret_cast<uint64_t>(f.k_base(is_new)), va = reinterpret_cast<uint64_t>(f.v_base(is_new));
     klo = scalar(unsigned(ka));
     khi = scalar(unsigned(ka >> 32));
     vlo = scalar(unsigned(va));
     vhi = scalar(unsigned(va >> 32));
-    stride = scalar(f.stride);
-    bytes = scalar(15 * f.stride + Layout<D>::ROWB);
+    stride = scalar(f.stride(is_new));
+    bytes = scalar(15 * f.stride(is_new) + Layout<D>::ROWB);
     slots = f.slots[0];
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      ko[i] = f.ko[0][i];
-      vo[i] = f.vo[0][i];
-    }
+    f.aim(0, f.stride(is_new), ko, vo);
   }
 };
 // Up to n tiles from the one that is on its way to buffer a.buf, each as Rows::tile does it; lane i of a.slots is the tile behind the first.  Returns 0, or
@@ -824,88 +756,78 @@ template <class T, int D>
 __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedParams p) {
   using L = Layout<D>;
   constexpr int KT = kManyKeys, ROWS = kManyRows, TILE = KT * L::ROWB;
+  static_assert(kStaged * sizeof(Entry) <= 4 * TILE, "the line's numbers lie where tiles will");
   __shared__ __attribute__((aligned(1024))) char tiles[4 * TILE];      // two buffers of K and V
   __shared__ int64_t scratch[kThreads / 64 + 2];
+  __shared__ RowNotes<32> notes[kThreads / 64];
   __shared__ int poison;                 // the last unit of which a page was none
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid == 0) poison = -1;
-  const Span sp = my_span<KT, ROWS>(p, scratch);
+  const Span sp = my_span<KT, ROWS>(p, reinterpret_cast<Entry *>(tiles), scratch);
   Note note{-1, 0};
   const unsigned lds0 = lds_address(tiles);
   int64_t at = sp.unit_at;
   for (int u = max(sp.unit, 0); u < p.units && at < sp.end; ++u) {
-    const Unit un = unit_of(p, u, ROWS);
+    const Unit un = unit_of(u, p.by_tiles, p.by_heads, ROWS);
     const Request r = request_of(p, un.b, un.h);
     if (un.row0 >= r.n * p.G) continue;
-    const RowRange x = row_range(p, r, un.row0, ROWS);
-    const Tiles<KT> tl = tiles_of<KT>(p, r, x);
+    const RowRange x = row_range(r, p.rules, un.row0, ROWS);
+    const Tiles<KT> tl = tiles_of<KT>(r, x, p.rules.keys);
     const int nt = tl.count();
-    int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
-    const bool owns = sp.begin <= at, begins = t0 == 0, ends = t1 == nt;
-    if (nt > 0) {
-      const int turn = int(sp.into_span(at) % nt);
-      t0 += turn;
-      t1 += turn;
-      if (t0 >= nt) {
-        t0 -= nt;
-        t1 -= nt;
-      }
-    }
+    const Piece pc = piece_of(sp.line, sp.begin, sp.end, at, nt, int64_t(nt) * 2 * TILE > kL2);
+    const int t0 = pc.t0, t1 = pc.t1;
     at += kUnitCost + nt;
-    if (t0 >= t1 && !(nt == 0 && owns)) continue;
+    if (!pc.is) continue;
 
     Rows<T, D, KT / 16, 2> rows;
     rows.clear();
-    Feed<D, KT, 1, 1> ld(p, r, tl, un.b, un.h, wave, t0);
     const int row0 = un.row0 + 32 * wave;
     if (t0 < t1) {
-      const RowRange mine = row_range(p, r, min(row0, r.n * p.G - 1), 32);
-      const FreeKeys seen = free_keys(r, mine);
-      // a wave without rows, or whose rows see none of the tile, has nothing to do
-      const int end_new = row0 < r.n * p.G ? mine.end1 : 0, end_hist = row0 < r.n * p.G ? INT32_MAX : 0;
-      int k0 = ld.k0;
-      bool is_new = ld.is_new;
-      ld.bring(lds0, lds0 + TILE, t1);
+      const RowRange mine = row_range(r, p.rules, min(row0, r.n * p.G - 1), 32);
+      const RangeKeys seen = range_keys(r, mine);
+      Feed<D, KT, 1, 1> ld(p, r, tl, seen, row0 < r.n * p.G, un.b, un.h, wave, t0, t1);
       rows.load_q(p, r, un.h, row0);
+      auto now = ld.bring(lds0, lds0 + TILE);
+      notes[wave].fill(p, r, row0);
       rows.settle();
       unsigned buf = lds0;
       for (int t = t0; t < t1; ++t) {
-        if (rows.all_set && ld.is_new == is_new && ld.k0 == k0 + KT && k0 < (is_new ? end_new : end_hist)) {
-          // tiles that all rows see, the one behind each a whole one of the same run
-          const int until = seen.until(k0, is_new), n = min(min((until - k0) / KT, ld.whole), min(t1 - 1 - t, 64 - ld.lane));
-          if (n > 0) {
-            SeenTiles<D> a;
-            a.place(lds0, buf == lds0 ? 0 : 1, wave, p.c);
-            a.rows_of(ld);
-            int lane_at = scalar(ld.lane);
-            const int due = seen_tiles<T, D>(a, rows.q, rows.o, rows.l, rows.minus_mc, lane_at, scalar(n));
-            const int begun = lane_at - ld.lane, done = begun - (due != 0);
-            ld.on(begun, t1);
-            t += done;
-            k0 += done * KT;
-            if (done & 1) buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
-            if (due) {
-              rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, due == 1 ? k0 : k0 + KT / 2, due == 1);
-              k0 += KT;
-              buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
-              continue;
-            }
+        unsigned other = buf == lds0 ? lds0 + 2 * TILE : lds0;
+        const int n = rows.all_set ? ld.steps(now) : 0;
+        int due = 0;
+        auto next = now;
+        if (n > 0) {
+          SeenTiles<D> a;
+          a.place(lds0, buf == lds0 ? 0 : 1, wave, p.c);
+          a.rows_of(ld);
+          int lane_at = scalar(ld.lane);
+          due = seen_tiles<T, D>(a, rows.q, rows.o, rows.l, rows.minus_mc, lane_at, scalar(n));
+          const int begun = lane_at - ld.lane, done = begun - (due != 0);
+          // the tile under way, or the one that is left to be done and the one that is under way behind it
+          next = ld.coming(lane_at - 1);
+          if (done > 0) now = ld.coming(lane_at - 1 - (due != 0));
+          ld.on(begun);
+          t += done;
+          if (done & 1) {
+            buf = other;
+            other = buf == lds0 ? lds0 + 2 * TILE : lds0;
           }
         }
-        // the wave's rows of this tile have landed, and every wave is done with the tile before
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const unsigned other = buf == lds0 ? lds0 + 2 * TILE : lds0;
-        const int next_k0 = ld.k0;
-        const bool next_new = ld.is_new;
-        if (t + 1 < t1) ld.bring(other, other + TILE, t1);
-        if (k0 < (is_new ? end_new : end_hist)) rows.tile(p, r, row0, buf, buf + TILE, k0, is_new, k0, k0 + KT <= seen.until(k0, is_new));
-        k0 = next_k0;
-        is_new = next_new;
+        if (!due) {
+          // the wave's rows of this tile have landed, and every wave is done with the tile before
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          if (t + 1 < t1) next = ld.bring(other, other + TILE);
+        }
+        if (now.seen != kNoneSeen)
+          rows.tile(p, r, notes[wave], buf, buf + TILE, now.k0, now.is_new, due == 2 ? now.k0 + KT / 2 : now.k0, due == 2 ? int(kSomeHidden) : now.seen);
+        now = next;
         buf = other;
       }
+      if (ld.met_bad()) poison = u;
+    } else if (r.bad) {
+      poison = u;
     }
-    if (ld.met_bad()) poison = u;
-    __syncthreads();                     // all waves are done with the tiles and have said what pages they met
+    lds_barrier();                       // all waves are done with the tiles and have said what pages they met
     const bool nan = poison == u;
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -914,7 +836,7 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
       l += __shfl_xor(l, 32);
       if (nan) l = NAN;
       const int row = row0 + 16 * qb + (lane & 15), g = lane >> 4;
-      if (begins && ends) {
+      if (pc.begins && pc.ends) {
         if (row < r.n * p.G) {
           const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -922,7 +844,7 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
           if (p.lse && g == 0) store_lse(p, r, un.h, row, rows.m[qb], l);
         }
       } else {
-        float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, begins);
+        float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, pc.begins);
         const int in_unit = row - un.row0;
 #pragma unroll
         for (int db = 0; db < L::CH / 2; ++db) *reinterpret_cast<f32x4 *>(slot + in_unit * D + 16 * db + 4 * g) = rows.o[db][qb];
@@ -932,9 +854,9 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
         }
       }
     }
-    if (begins && !ends) note.tail_unit = u;
-    if (!begins) note.head = ends ? 2 : 1;
-    __syncthreads();                     // the poison of this piece has been read, the tiles may be loaded again
+    if (pc.begins && !pc.ends) note.tail_unit = u;
+    if (!pc.begins) note.head = pc.ends ? 2 : 1;
+    lds_barrier();                       // the poison of this piece has been read, the tiles may be loaded again
   }
   if (!p.whole && tid == 0) reinterpret_cast<Note *>(p.ws)[sp.index] = note;
 }
@@ -951,58 +873,55 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
   __shared__ __attribute__((aligned(1024))) char tiles[kFewWaves][RING][2][TILE];
   __shared__ int64_t scratch[kThreads / 64 + 2];
   __shared__ float stats[kFewWaves][2][ROWS];
+  __shared__ RowNotes<ROWS> notes[kFewWaves];
   __shared__ int poison;                 // the last unit of which a page was none
+  static_assert(kStaged * sizeof(Entry) <= sizeof(tiles), "the line's numbers lie where tiles will");
   static_assert(sizeof(float) * ROWS * D <= sizeof(tiles[0]), "a wave's sums pass through its tiles");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (tid == 0) poison = -1;
-  const Span sp = my_span<KT, ROWS>(p, scratch);
+  const Span sp = my_span<KT, ROWS>(p, reinterpret_cast<Entry *>(tiles), scratch);
   Note note{-1, 0};
   const unsigned lds0 = lds_address(&tiles[wave][0][0][0]);
   int64_t at = sp.unit_at;
   for (int u = max(sp.unit, 0); u < p.units && at < sp.end; ++u) {
-    const Unit un = unit_of(p, u, ROWS);
+    const Unit un = unit_of(u, p.by_tiles, p.by_heads, ROWS);
     const Request r = request_of(p, un.b, un.h);
     if (un.row0 >= r.n * p.G) continue;
-    const RowRange x = row_range(p, r, un.row0, ROWS);
-    const Tiles<KT> tl = tiles_of<KT>(p, r, x);
+    const RowRange x = row_range(r, p.rules, un.row0, ROWS);
+    const Tiles<KT> tl = tiles_of<KT>(r, x, p.rules.keys);
     const int nt = tl.count();
-    const int t0 = cut_at(sp.begin - at, nt), t1 = at + kUnitCost + nt <= sp.end ? nt : cut_at(sp.end - at, nt);
-    const bool owns = sp.begin <= at;
+    const Piece pc = piece_of(sp.line, sp.begin, sp.end, at, nt, false);
+    const int t0 = pc.t0, t1 = pc.t1;
     at += kUnitCost + nt;
-    if (t0 >= t1 && !(nt == 0 && owns)) continue;
+    if (!pc.is) continue;
 
     Rows<T, D, 2, QB> rows;
     rows.clear();
     int t = t0 + wave;
-    Feed<D, KT, 2, kFewWaves> ld(p, r, tl, un.b, un.h, 0, max(min(t, t1 - 1), 0));
-    const FreeKeys seen = free_keys(r, x);
-    // where the tiles that are under way begin: this one's and the next one's
-    int k0 = ld.k0, next_k0 = 0;
-    bool is_new = ld.is_new, next_new = false;
-    if (t < t1) ld.bring(lds0, lds0 + TILE, t1);
-    if (t + kFewWaves < t1) {
-      next_k0 = ld.k0;
-      next_new = ld.is_new;
-      ld.bring(lds0 + 2 * TILE, lds0 + 3 * TILE, t1);
-    }
-    rows.load_q(p, r, un.h, un.row0);
-    rows.settle();
-    for (unsigned buf = lds0; t < t1; t += kFewWaves) {
-      // this tile has landed, the next one may still be on its way
-      if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      rows.tile(p, r, un.row0, buf, buf + TILE, k0, is_new, k0, k0 + KT <= seen.until(k0, is_new));
-      k0 = next_k0;
-      is_new = next_new;
-      if (t + 2 * kFewWaves < t1) {
-        next_k0 = ld.k0;
-        next_new = ld.is_new;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the reads of this buffer are done
-        ld.bring(buf, buf + TILE, t1);
+    if (t < t1) {
+      const RangeKeys seen = range_keys(r, x);
+      Feed<D, KT, 2, kFewWaves> ld(p, r, tl, seen, true, un.b, un.h, 0, t, t1);
+      rows.load_q(p, r, un.h, un.row0);
+      notes[wave].fill(p, r, un.row0);
+      auto now = ld.bring(lds0, lds0 + TILE), next = now;
+      if (t + kFewWaves < t1) next = ld.bring(lds0 + 2 * TILE, lds0 + 3 * TILE);
+      rows.settle();
+      for (unsigned buf = lds0; t < t1; t += kFewWaves) {
+        // this tile has landed, the next one may still be on its way
+        if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (now.seen != kNoneSeen) rows.tile(p, r, notes[wave], buf, buf + TILE, now.k0, now.is_new, now.k0, now.seen);
+        now = next;
+        if (t + 2 * kFewWaves < t1) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the reads of this buffer are done
+          next = ld.bring(buf, buf + TILE);
+        }
+        buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
       }
-      buf = buf == lds0 ? lds0 + 2 * TILE : lds0;
+      if (ld.met_bad()) poison = u;
+    } else if (r.bad) {
+      poison = u;
     }
-    if (ld.met_bad()) poison = u;
     // the four waves' sums meet in LDS: references, row sums, outputs
     float *mine = reinterpret_cast<float *>(&tiles[wave][0][0][0]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -1019,9 +938,9 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
         stats[wave][1][row] = l;
       }
     }
-    __syncthreads();
-    const bool nan = poison == u, whole = t0 == 0 && t1 == nt;
-    float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, t0 == 0);
+    lds_barrier();
+    const bool nan = poison == u, whole = pc.begins && pc.ends;
+    float *slot = PartialSlot<ROWS, D>::of(p.ws, sp.index, pc.begins);
     for (int i = tid; i < ROWS * D / 4; i += kThreads) {
       const int in_unit = i / (D / 4), col = 4 * (i % (D / 4)), row = un.row0 + in_unit;
       if (row >= r.n * p.G) continue;
@@ -1049,9 +968,9 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
         }
       }
     }
-    if (t0 == 0 && t1 < nt) note.tail_unit = u;
-    if (t0 > 0) note.head = t1 == nt ? 2 : 1;
-    __syncthreads();                     // the tiles may be loaded again
+    if (pc.begins && !pc.ends) note.tail_unit = u;
+    if (!pc.begins) note.head = pc.ends ? 2 : 1;
+    lds_barrier();                       // the tiles may be loaded again
   }
   if (!p.whole && tid == 0) reinterpret_cast<Note *>(p.ws)[sp.index] = note;
 }
@@ -1068,7 +987,7 @@ __global__ __launch_bounds__(kMergeThreads) void df_paged_merge_kernel(const Pag
   const Note *notes = reinterpret_cast<const Note *>(p.ws);
   const int w0 = blockIdx.x, u = notes[w0].tail_unit;
   if (u < 0 || u >= p.units) return;
-  const Unit un = unit_of(p, u, ROWS);
+  const Unit un = unit_of(u, p.by_tiles, p.by_heads, ROWS);
   const Request r = request_of(p, un.b, un.h);
   const int in_unit = blockIdx.y * RPB + threadIdx.x / V, row = un.row0 + in_unit, col = 4 * (threadIdx.x % V);
   if (row >= r.n * p.G) return;
@@ -1186,9 +1105,12 @@ extern "C" df_status df_paged_attn(const df_paged_attn_args *a, void *stream) {
   p.cap_stride = c->cap_stride;
   p.B = c->B; p.Hkv = c->H_kv; p.Hq = a->H_q; p.G = G;
   p.page_log2 = log2_of(c->page_tokens); p.n_pages = c->n_pages; p.max_pages = c->max_pages;
-  p.total = a->total_new; p.max_new = a->max_new; p.block = a->block;
+  p.total = a->total_new; p.max_new = a->max_new;
+  p.rules = Rules{Divider::by(G), Divider::by(a->block), a->k_cur != nullptr};
   p.row_tiles = int(row_tiles);
   p.units = int(units);
+  p.by_tiles = Divider::by(p.row_tiles);
+  p.by_heads = Divider::by(c->H_kv);
   p.c = a->softmax_scale * 1.4426950408889634f;
   p.ln_unit = float(double(a->softmax_scale) / double(p.c));
   p.ws = static_cast<char *>(a->workspace);

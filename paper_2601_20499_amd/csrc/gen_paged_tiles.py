@@ -16,7 +16,7 @@ with DEPTH of them in flight, each waited for by count.  Before the products of 
 
 Why asm: written in C++ the compiler read most operands right before their use (a wait of 64 to 128 cycles each), and took 250 vector
 and 100 scalar instructions a tile besides the products where 112 and 45 do.  1280x720 chunk and twelve cached frames: 3509 us in
-C++, MFMA_US here.
+C++, 2990 us here (before its workgroups shared tiles in L2).
 
 The statement carries its own waits and wait states (the compiler's hazard recogniser does not look into asm):
   * a vector instruction keeps 8 wait states from a product whose result it reads: at least nine instructions lie between the last
@@ -196,9 +196,65 @@ __device__ __forceinline__ int seen_tiles<{T}, {D}>(const SeenTiles<{D}> &a, con
 """
 
 
+def operands(lines, ops, depth):
+    """The operands' reads, `depth` of them ahead, and the products of each behind the wait for it."""
+    slot = lambda i: STAGE + 4 * (i % DEPTH)
+
+    def issue(i):
+        if i < len(ops):
+            w = 4 // len(ops[i][0])
+            for k, r in enumerate(ops[i][0]):
+                lines.append(r.replace("@", f"v[{slot(i) + w * k}:{slot(i) + w * k + w - 1}]"))
+
+    for i in range(depth):
+        issue(i)
+    for i, (_, products) in enumerate(ops):
+        lines.append(f"s_waitcnt lgkmcnt({sum(len(o[0]) for o in ops[i + 1:i + depth])})")
+        lines += [m.replace("@", quad(slot(i))) for m in products]
+        issue(i + depth)
+    return lines + ["s_nop 7", "s_nop 7"]
+
+
+def one_product(D, fp16, second):
+    """S^T = K Q^T or O^T += V^T P^T of a whole tile by itself, for tiles with something between the two."""
+    rowb, KS, DB = 2 * D, D // 32, D // 16
+    mfma = "v_mfma_f32_16x16x32_f16" if fp16 else "v_mfma_f32_16x16x32_bf16"
+    T = "Fp16" if fp16 else "Bf16"
+    if second:
+        ops = [([f"ds_read_b64_tr_b16 @, %[v{db}] offset:{(32 * h + 4 * u) * rowb}" for u in range(2)],
+                [f"{mfma} {quad(O[db, qb])}, @, {quad(P[h, qb])}, {quad(O[db, qb])}" for qb in range(2)])
+               for h in range(2) for db in range(DB)]
+        outs = [f'"+{{{quad(O[db, qb])}}}"(o[{db}][{qb}])' for db in range(DB) for qb in range(2)]
+        ins = [f'"{{{quad(P[h, qb])}}}"(w[{h}][{qb}])' for h in range(2) for qb in range(2)]
+        ins += [f'[v{db}] "v"(first ^ {32 * db}u)' for db in range(DB)]
+        head = f"void values_of<{T}, {D}>(unsigned first, const s16x8 (&w)[2][2], f32x4 (&o)[{DB}][2])"
+        lines = ["s_waitcnt lgkmcnt(0)", "s_nop 1"]
+    else:
+        ops = [([f"ds_read_b128 @, %[k{ks}] offset:{(32 * (kb // 2) + 4 * (kb % 2)) * rowb}"],
+                [f"{mfma} {quad(S[kb, qb])}, @, {quad(Q[ks, qb])}, {quad(S[kb, qb]) if ks else 0}" for qb in range(2)])
+               for ks in range(KS) for kb in range(4)]
+        outs = [f'"=&{{{quad(S[kb, qb])}}}"(s[{kb}][{qb}])' for kb in range(4) for qb in range(2)]
+        ins = [f'"{{{quad(Q[ks, qb])}}}"(q[{ks}][{qb}])' for ks in range(KS) for qb in range(2)]
+        ins += [f'[k{ks}] "v"(first ^ {64 * ks}u)' for ks in range(KS)]
+        head = f"void scores_of<{T}, {D}>(unsigned first, const s16x8 (&q)[{KS}][2], f32x4 (&s)[4][2])"
+        lines = ["s_waitcnt lgkmcnt(0)"]
+    body = "\n".join(f'      "{x}\\n\\t"' for x in operands(lines, ops, DEPTH))
+    clob = ['"memory"'] + [f'"v{r}"' for r in range(STAGE, 256)]
+    return f"""template <>
+__device__ __forceinline__ {head} {{
+  asm volatile(
+{body}
+      : {', '.join(outs)}
+      : {', '.join(ins)}
+      : {', '.join(clob)});
+}}
+"""
+
+
 def text():
     head = "// Generated by gen_paged_tiles.py - do not edit; see that script for the schedule and its reasons.\n"
-    return head + "\n".join(statement(D, fp16) for D in (128, 64) for fp16 in (False, True))
+    every = [(D, fp16) for D in (128, 64) for fp16 in (False, True)]
+    return head + "\n".join([statement(*x) for x in every] + [one_product(*x, second) for x in every for second in (False, True)])
 
 
 OUT = os.path.join(os.path.dirname(os.path.abspath(__file__)), "df_paged_tiles.inc")
