@@ -6,6 +6,8 @@ host bookkeeping arrays as ctypes arrays.  There is no CPU fallback: if the
 HIP library is missing the import of this module fails.  The calls of a generation loop go through a small extension
 (csrc/df_marshal.cpp) that marshals the ordinary kinds of arguments in native code: attention of 64 queries is issued in 3.7 us
 instead of 8.8, of 1170 in 4.7 instead of 9.4, a small append in 3.1 instead of 5.2, a small pack in 3.3 instead of 6.9.
+A step of single tokens over a paged cache: slots in 7.8 us (the kernel's time) instead of 12.9, append in 4.0 instead of 10.5, attention of
+short histories in 12.7 instead of 18.
 """
 from __future__ import annotations
 
@@ -181,6 +183,7 @@ def _marshal():
         from . import _marshal as native
         native.setup(*(C.cast(getattr(lib, n), C.c_void_p).value for n in
                        ("df_attn_fwd", "df_attn_fwd_static", "df_head_score", "df_kv_append", "df_pack_context")))
+        native.setup_paged(*(C.cast(getattr(lib, n), C.c_void_p).value for n in ("df_page_map", "df_paged_append", "df_paged_attn")))
         _native = native
     except ImportError:
         _native = False
@@ -498,6 +501,12 @@ class PagedCache:
         self._i32, self._i64, self._u8, self._f32 = torch.int32, torch.int64, torch.uint8, torch.float32
         self.ref = C.pointer(self.c)
 
+    def _is_here(self):
+        """Kernels run on the current GPU, which need not be able to read another's memory."""
+        if self.device.type == "cuda":
+            import torch
+            _want(self.device.index == torch.cuda.current_device(), f"the cache is on {self.device}, not on the current GPU")
+
     def _rows(self, t, heads: int, what: str):
         """[tokens, heads, d] in any token and head strides, d contiguous; strides of dimensions of one do not matter."""
         _want(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.d and t.dtype == self.dtype and t.device == self.device,
@@ -511,11 +520,17 @@ def df_page_map(cache: PagedCache, cu_new, slot_map, status, release=None, len_o
     """cu_new [B+1] int32, slot_map [total, H_kv] int64, status [1] int32, release [B] uint8 or None; len_out and n_free_out are the
     cache's own length and n_free where they are not given."""
     dev = cache.device
+    len_out = cache.length if len_out is None else len_out
+    n_free_out = cache.n_free if n_free_out is None else n_free_out
+    native = _native if _native is not None else _marshal()
+    if native:
+        done = native.page_map(cache, cu_new, slot_map, status, release, len_out, n_free_out, stream)
+        if done is not None:
+            return _check(done, "df_page_map")
+    cache._is_here()
     _like(cu_new, cache._i32, (cache.B + 1,), dev, "cu_new")
     _like(slot_map, cache._i64, (slot_map.shape[0], cache.Hkv), dev, "slot_map")
     _like(status, cache._i32, (1,), dev, "status")
-    len_out = cache.length if len_out is None else len_out
-    n_free_out = cache.n_free if n_free_out is None else n_free_out
     _like(len_out, cache._i32, (cache.B,), dev, "len_out")
     _like(n_free_out, cache._i32, (1,), dev, "n_free_out")
     if release is not None:
@@ -529,6 +544,12 @@ def df_page_map(cache: PagedCache, cu_new, slot_map, status, release=None, len_o
 
 def df_paged_append(cache: PagedCache, k_new, v_new, slot_map, stream=None):
     """k_new, v_new [total, H_kv, d] (any token and head strides), slot_map [total, H_kv] int64 from df_page_map."""
+    native = _native if _native is not None else _marshal()
+    if native:
+        status = native.paged_append(cache, k_new, v_new, slot_map, stream)
+        if status is not None:
+            return _check(status, "df_paged_append")
+    cache._is_here()
     tok, head = cache._rows(k_new, cache.Hkv, "k_new")
     _want(cache._rows(v_new, cache.Hkv, "v_new") == (tok, head) and v_new.shape == k_new.shape, "v_new: not laid out as k_new")
     _like(slot_map, cache._i64, (k_new.shape[0], cache.Hkv), cache.device, "slot_map")
@@ -548,6 +569,12 @@ def df_paged_attn(q, k_cur, v_cur, cache: PagedCache, cu_new, out, softmax_scale
     """q, out [total, H_q, d], k_cur, v_cur [total, H_kv, d] (any token and head strides) or both None; cu_new [B+1] int32; lse_out
     [H_q, total] fp32.  block: tokens of a causal block (1: token by token; at least the longest request's: all see all); max_new: the
     most new tokens that a request has (default: all of them)."""
+    native = _native if _native is not None else _marshal()
+    if native:
+        status = native.paged_attn(q, k_cur, v_cur, cache, cu_new, out, softmax_scale, block, max_new, lse_out, workspace, stream)
+        if status is not None:
+            return _check(status, "df_paged_attn")
+    cache._is_here()
     H_q, total = q.shape[1], q.shape[0]
     a = df_paged_attn_args()
     a.cache = cache.ref

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -20,6 +21,9 @@ decltype(&df_attn_fwd) attn_fwd, attn_fwd_static;
 decltype(&df_head_score) head_score;
 decltype(&df_kv_append) kv_append;
 decltype(&df_pack_context) pack_context;
+decltype(&df_page_map) page_map_entry;
+decltype(&df_paged_append) paged_append_entry;
+decltype(&df_paged_attn) paged_attn_entry;
 
 // The readers below say whether an argument is of the ordinary kind.  (Nothing is thrown where it is not: that took 3 to 5 us, a third to a half of
 // what a call costs that is marshalled in Python, such as one with a torch.cuda.Stream.)
@@ -219,6 +223,114 @@ PyObject *append(PyObject *, PyObject *const *x, Py_ssize_t n) {
   });
 }
 
+// A binding.PagedCache: its C struct, and its pages for their type and place; no cache where it is no such object or not on the current GPU.
+struct PagedOf {
+  Py_buffer view{};
+  df_paged_cache *cache = nullptr;
+  at::ScalarType type{};
+  c10::Device device{c10::kCPU};
+  explicit PagedOf(PyObject *x) {
+    PyObject *c = PyObject_GetAttrString(x, "c"), *k = c ? PyObject_GetAttrString(x, "k_pages") : nullptr;
+    const at::Tensor *pages = k ? tensor(k) : nullptr;
+    if (c == nullptr || k == nullptr || PyObject_GetBuffer(c, &view, PyBUF_WRITABLE) != 0) PyErr_Clear();
+    else if (pages && size_t(view.len) == sizeof(df_paged_cache)) {
+      type = pages->scalar_type();
+      device = pages->device();
+      if (device.index() == c10::hip::current_device()) cache = static_cast<df_paged_cache *>(view.buf);
+    }
+    Py_XDECREF(k);                   // the object holds it
+    Py_XDECREF(c);                   // the view holds it
+  }
+  PagedOf(const PagedOf &) = delete;
+  ~PagedOf() { PyBuffer_Release(&view); }
+
+  // An array of the cache's device: its address, null for an empty one.
+  template <class T>
+  bool array(PyObject *x, at::ScalarType t, std::initializer_list<int64_t> shape, T *&to) const {
+    const at::Tensor *a = tensor(x);
+    if (!a || a->scalar_type() != t || a->device() != device || !a->sizes().equals(shape) || !a->is_contiguous()) return false;
+    to = static_cast<T *>(address(*a));
+    return true;
+  }
+  // Rows [tokens, heads, d] of the cache's type; strides of dimensions of one do not matter.
+  bool rows(const at::Tensor *t, int64_t heads, int64_t &tok, int64_t &head) const {
+    if (!t || t->dim() != 3 || t->size(1) != heads || t->size(2) != cache->d || t->scalar_type() != type || t->device() != device || t->stride(2) != 1)
+      return false;
+    tok = t->size(0) > 1 ? t->stride(0) : heads * cache->d;
+    head = heads > 1 ? t->stride(1) : cache->d;
+    return true;
+  }
+};
+
+// cache, cu_new, slot_map, status, release, len_out, n_free_out, stream
+PyObject *page_map(PyObject *, PyObject *const *x, Py_ssize_t n) {
+  return or_none(n, 8, [&]() -> PyObject * {
+    const at::Tensor *slots = tensor(x[2], 2);
+    df_page_map_args a{};
+    void *st;
+    if (!slots || !stream(x[7], st) || !size32(slots->size(0), a.total_new)) return nullptr;
+    const PagedOf p(x[0]);
+    if (!p.cache) return nullptr;
+    const int64_t B = p.cache->B;
+    if (!p.array(x[1], at::kInt, {B + 1}, a.cu_new) || !p.array(x[2], at::kLong, {a.total_new, p.cache->H_kv}, a.slot_map) ||
+        !p.array(x[3], at::kInt, {1}, a.status) || (x[4] != Py_None && !p.array(x[4], at::kByte, {B}, a.release)) ||
+        !p.array(x[5], at::kInt, {B}, a.len_out) || !p.array(x[6], at::kInt, {1}, a.n_free_out))
+      return nullptr;
+    a.cache = p.cache;
+    return PyLong_FromLong(without_gil([&] { return page_map_entry(&a, st); }));
+  });
+}
+
+// cache, k_new, v_new, slot_map, stream
+PyObject *paged_append(PyObject *, PyObject *const *x, Py_ssize_t n) {
+  return or_none(n, 5, [&]() -> PyObject * {
+    const at::Tensor *k = tensor(x[1], 3), *v = tensor(x[2], 3);
+    df_paged_append_args a{};
+    void *st;
+    int64_t tok, head;
+    if (!k || !v || !stream(x[4], st) || !size32(k->size(0), a.total_new)) return nullptr;
+    const PagedOf p(x[0]);
+    if (!p.cache || !p.rows(k, p.cache->H_kv, a.stride_tok, a.stride_head) || !p.rows(v, p.cache->H_kv, tok, head) || tok != a.stride_tok ||
+        head != a.stride_head || v->size(0) != k->size(0) || !p.array(x[3], at::kLong, {a.total_new, p.cache->H_kv}, a.slot_map))
+      return nullptr;
+    a.cache = p.cache;
+    a.k_new = address(*k);
+    a.v_new = address(*v);
+    return PyLong_FromLong(without_gil([&] { return paged_append_entry(&a, st); }));
+  });
+}
+
+// q, k_cur, v_cur, cache, cu_new, out, softmax_scale, block, max_new, lse_out, workspace, stream
+PyObject *paged_attn(PyObject *, PyObject *const *x, Py_ssize_t n) {
+  return or_none(n, 12, [&]() -> PyObject * {
+    const at::Tensor *q = tensor(x[0], 3), *out = tensor(x[5], 3);
+    df_paged_attn_args a{};
+    void *st;
+    if (!q || !out || !stream(x[11], st) || !size32(q->size(0), a.total_new) || !size32(q->size(1), a.H_q) || !real(x[6], a.softmax_scale) ||
+        !number(x[7], a.block) || !(x[8] == Py_None || number(x[8], a.max_new)) || !buffer_or_null(x[10], a.workspace, a.workspace_bytes))
+      return nullptr;
+    if (x[8] == Py_None) a.max_new = a.total_new;
+    const PagedOf p(x[3]);
+    if (!p.cache || !p.rows(q, a.H_q, a.q_stride_tok, a.q_stride_head) || !p.rows(out, a.H_q, a.o_stride_tok, a.o_stride_head) ||
+        out->size(0) != a.total_new || !p.array(x[4], at::kInt, {int64_t(p.cache->B) + 1}, a.cu_new) ||
+        (x[9] != Py_None && !p.array(x[9], at::kFloat, {a.H_q, a.total_new}, a.lse_out)))
+      return nullptr;
+    if (x[1] != Py_None || x[2] != Py_None) {
+      const at::Tensor *k = tensor(x[1], 3), *v = tensor(x[2], 3);
+      int64_t tok, head;
+      if (!p.rows(k, p.cache->H_kv, a.kc_stride_tok, a.kc_stride_head) || !p.rows(v, p.cache->H_kv, tok, head) || tok != a.kc_stride_tok ||
+          head != a.kc_stride_head || k->size(0) != a.total_new || v->size(0) != a.total_new)
+        return nullptr;
+      a.k_cur = address(*k);
+      a.v_cur = address(*v);
+    }
+    a.cache = p.cache;
+    a.q = address(*q);
+    a.out = address(*out);
+    return PyLong_FromLong(without_gil([&] { return paged_attn_entry(&a, st); }));
+  });
+}
+
 template <class T>
 PyObject *list_of(const T *x, int n) {
   PyObject *list = PyList_New(n);
@@ -264,20 +376,26 @@ PyObject *pack(PyObject *, PyObject *const *x, Py_ssize_t n) {
   });
 }
 
-// Addresses of df_attn_fwd, df_attn_fwd_static, df_head_score, df_kv_append and df_pack_context in the library that the binding loaded.
-PyObject *setup(PyObject *, PyObject *const *x, Py_ssize_t n) {
-  void *f[5];
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "five addresses");
-    return nullptr;
+// The addresses of N functions.
+template <int N>
+bool addresses(PyObject *const *x, Py_ssize_t n, void *(&f)[N]) {
+  if (n != N) {
+    PyErr_Format(PyExc_TypeError, "%d addresses", N);
+    return false;
   }
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < N; ++i) {
     f[i] = PyLong_AsVoidPtr(x[i]);
     if (f[i] == nullptr) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a function has no address");
-      return nullptr;
+      return false;
     }
   }
+  return true;
+}
+// Addresses of df_attn_fwd, df_attn_fwd_static, df_head_score, df_kv_append and df_pack_context in the library that the binding loaded.
+PyObject *setup(PyObject *, PyObject *const *x, Py_ssize_t n) {
+  void *f[5];
+  if (!addresses(x, n, f)) return nullptr;
   attn_fwd = reinterpret_cast<decltype(attn_fwd)>(f[0]);
   attn_fwd_static = reinterpret_cast<decltype(attn_fwd_static)>(f[1]);
   head_score = reinterpret_cast<decltype(head_score)>(f[2]);
@@ -285,12 +403,23 @@ PyObject *setup(PyObject *, PyObject *const *x, Py_ssize_t n) {
   pack_context = reinterpret_cast<decltype(pack_context)>(f[4]);
   Py_RETURN_NONE;
 }
+// Those of df_page_map, df_paged_append and df_paged_attn.
+PyObject *setup_paged(PyObject *, PyObject *const *x, Py_ssize_t n) {
+  void *f[3];
+  if (!addresses(x, n, f)) return nullptr;
+  page_map_entry = reinterpret_cast<decltype(page_map_entry)>(f[0]);
+  paged_append_entry = reinterpret_cast<decltype(paged_append_entry)>(f[1]);
+  paged_attn_entry = reinterpret_cast<decltype(paged_attn_entry)>(f[2]);
+  Py_RETURN_NONE;
+}
 
 template <class F>
 PyCFunction as_c(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 PyMethodDef methods[] = {{"setup", as_c(setup), METH_FASTCALL, nullptr},   {"attn", as_c(attn), METH_FASTCALL, nullptr},
                          {"score", as_c(score), METH_FASTCALL, nullptr},   {"append", as_c(append), METH_FASTCALL, nullptr},
-                         {"pack", as_c(pack), METH_FASTCALL, nullptr},     {nullptr, nullptr, 0, nullptr}};
+                         {"pack", as_c(pack), METH_FASTCALL, nullptr},     {"setup_paged", as_c(setup_paged), METH_FASTCALL, nullptr},
+                         {"page_map", as_c(page_map), METH_FASTCALL, nullptr}, {"paged_append", as_c(paged_append), METH_FASTCALL, nullptr},
+                         {"paged_attn", as_c(paged_attn), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
