@@ -27,6 +27,7 @@
 // unit that a span's end cuts leaves partial sums in the workspace; a second kernel puts them together.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "df_paged.h"
 
@@ -977,8 +978,10 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
 
 // ---- cut units ------------------------------------------------------------------------------------------------------------------------
 
-// Workgroup (w, y): if span w begins a unit that it does not end, rows y * kMergeRows ... of it are put together from its slot 1 and slot 0
-// of the spans behind it, up to the one that holds the unit's end.
+// Workgroup (w, y): if span w begins a unit that it does not end, rows y * RPB ... of it are put together from its slot 1 and slot 0
+// of the spans behind it, up to the one that holds the unit's end.  Bound by trips to memory: the end is looked for by 64 lanes at once, and the pieces' references
+// and sums are read several at a time, first all references (their largest is the unit's), then the sums.  A piece after the other, one token of 32
+// pieces took 12 us.
 constexpr int kMergeThreads = 256;
 
 template <class T, int D, int ROWS, int KT>
@@ -987,25 +990,60 @@ __global__ __launch_bounds__(kMergeThreads) void df_paged_merge_kernel(const Pag
   const Note *notes = reinterpret_cast<const Note *>(p.ws);
   const int w0 = blockIdx.x, u = notes[w0].tail_unit;
   if (u < 0 || u >= p.units) return;
+  int last = w0;
+  for (bool found = false; !found && last + 1 < spans;) {
+    const int w = last + 1 + (threadIdx.x & 63);
+    const uint64_t ends = __builtin_amdgcn_ballot_w64(w < spans && notes[min(w, spans - 1)].head != 1);
+    found = ends != 0;
+    last = min(last + (found ? 1 + __builtin_ctzll(ends) : 64), spans - 1);
+  }
   const Unit un = unit_of(u, p.by_tiles, p.by_heads, ROWS);
   const Request r = request_of(p, un.b, un.h);
   const int in_unit = blockIdx.y * RPB + threadIdx.x / V, row = un.row0 + in_unit, col = 4 * (threadIdx.x % V);
   if (row >= r.n * p.G) return;
-  const float *slot = PartialSlot<ROWS, D>::of(p.ws, w0, 1);
-  float m = slot[ROWS * D + in_unit], l = slot[ROWS * (D + 1) + in_unit];
-  f32x4 o = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
-  for (int w = w0 + 1; w < spans; ++w) {
-    const int head = notes[w].head;
-    slot = PartialSlot<ROWS, D>::of(p.ws, w, 0);
-    const float m1 = slot[ROWS * D + in_unit], l1 = slot[ROWS * (D + 1) + in_unit];
-    const f32x4 o1 = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
-    const float t = fmaxf(m, m1);
-    const float f0 = m == t ? 1.f : __builtin_amdgcn_exp2f((m - t) * p.c), f1 = m1 == t ? 1.f : __builtin_amdgcn_exp2f((m1 - t) * p.c);
-    m = t;
-    l = f0 * l + f1 * l1;
-    o = f0 * o + f1 * o1;
-    if (head != 1) break;
-  }
+  const float *slot = PartialSlot<ROWS, D>::of(p.ws, w0, 1), *head = PartialSlot<ROWS, D>::of(p.ws, 0, 0);
+  constexpr size_t kApart = 2 * PartialSlot<ROWS, D>::kFloats;
+  const float m0 = slot[ROWS * D + in_unit], l0 = slot[ROWS * (D + 1) + in_unit];
+  const f32x4 o0 = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
+  float m = m0, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  // REFS references and SUMS pieces of sums are read at once (behind the last: the last again, not counted).
+  const auto fold = [&](auto refs, auto sums) {
+    constexpr int REFS = decltype(refs)::value, SUMS = decltype(sums)::value;
+    for (int w = w0 + 1; w <= last; w += REFS) {
+      float x[REFS];
+#pragma unroll
+      for (int i = 0; i < REFS; ++i) x[i] = head[min(w + i, last) * kApart + ROWS * D + in_unit];
+#pragma unroll
+      for (int i = 0; i < REFS; ++i) m = fmaxf(m, x[i]);
+    }
+    const auto share = [&](float x) { return x == m ? 1.f : __builtin_amdgcn_exp2f((x - m) * p.c); };    // (minus infinity: no NaN)
+    l = share(m0) * l0;
+    o = share(m0) * o0;
+    for (int w = w0 + 1; w <= last; w += SUMS) {
+      float x[SUMS], l1[SUMS];
+      f32x4 o1[SUMS];
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i) {
+        slot = head + min(w + i, last) * kApart;
+        x[i] = slot[ROWS * D + in_unit];
+        l1[i] = slot[ROWS * (D + 1) + in_unit];
+        o1[i] = *reinterpret_cast<const f32x4 *>(slot + in_unit * D + col);
+      }
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i) {
+        const bool is = w + i <= last;
+        const float f = share(x[i]);
+        l = is ? l + f * l1[i] : l;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = is ? o[k] + f * o1[i][k] : o[k];
+      }
+    }
+  };
+  // Units of many rows mostly have two or three pieces, a long history of few rows has dozens (one token of 131072 keys: 14 us with 8 at a
+  // time, 7 with these; for a batch of single tokens, which has up to 8 pieces, the larger numbers cost 2 us more than they save).
+  if (ROWS != kManyRows && last - w0 > 8) fold(std::integral_constant<int, 32>(), std::integral_constant<int, 16>());
+  else fold(std::integral_constant<int, ROWS == kManyRows ? 4 : 8>(), std::integral_constant<int, ROWS == kManyRows ? 4 : 8>());
   store_row4<T>(p, r, un.h, row, col, o * (l == 0.f ? 0.f : 1.f / l));
   if (p.lse && col == 0) store_lse(p, r, un.h, row, m, l);
 }
@@ -1072,7 +1110,7 @@ extern "C" df_status df_paged_attn(const df_paged_attn_args *a, void *stream) {
   if (a->H_q <= 0 || a->total_new <= 0 || a->max_new <= 0 || a->block <= 0 || a->H_q % c->H_kv) return DF_ERR_SHAPE;
   if (a->H_q / c->H_kv > 64) return DF_ERR_UNSUPPORTED;
   if (a->max_new > a->total_new) return DF_ERR_SHAPE;
-  if (!(a->softmax_scale > 0.f) || !std::isfinite(a->softmax_scale)) return DF_ERR_RANGE;
+  if (!(a->softmax_scale > 0.f) || !std::isfinite(a->softmax_scale * 1.4426950408889634f)) return DF_ERR_RANGE;
   if (a->total_new > kMaxLen || !sizes_ok(a->H_q, c->H_kv, c->d, a->max_new)) return DF_ERR_RANGE;
   if (!aligned16(a->q) || !aligned16(a->out) || !stride_ok(a->q_stride_tok) || !stride_ok(a->o_stride_tok) ||
       (a->H_q > 1 && (!stride_ok(a->q_stride_head) || !stride_ok(a->o_stride_head))))

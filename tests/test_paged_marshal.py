@@ -35,3 +35,10 @@ def test_a_cache_of_another_gpu_is_refused(monkeypatch):
                  lambda: df.df_paged_attn(b.q, None, None, cache, b.cu, b.q, 0.125)):
         with pytest.raises(ValueError, match="not on the current GPU"):
             call()
+
+
+def test_a_scale_that_leaves_32_bits_is_refused():
+    """The kernels work with the scale times log2(e)."""
+    from tests import test_paged_abi as abi
+    for scale, code in ((3e38, df.DF_ERR_RANGE), (2e38, df.DF_ERR_WORKSPACE)):
+        assert abi._calls(df, abi._cache(df), softmax_scale=scale, workspace=None)[2]() == code
