@@ -209,7 +209,10 @@ struct Order {
 // ---- sharing out -------------------------------------------------------------------------------------------------------------
 // The units' costs (tiles + a constant) form a line, requests outermost, then key heads, then tiles of rows (neighbours read the same keys); it is
 // cut into equal spans.
-constexpr int kUnitCost = 4;           // cost of a unit besides its tiles, in tiles
+// Cost of a unit besides its tiles, in tiles: its request, pages and queries are fetched one after the other, and its hidden tiles take longer than
+// others.  4, 10, 16, 24: single tokens 236, 206, 204, 206 us, prompt pieces 506, 471, 462, 495, 390-token frames 87, 77, 80, 79,
+// 480p chunks 640, 634, 643, 654.
+constexpr int kUnitCost = 10;
 constexpr int kSnap = 3;               // no piece of a cut unit has fewer tiles ...
 constexpr int kMinSpan = 8;            // ... than fit into the shortest span; units of up to kMinSpan tiles are not cut
 static_assert(2 * kSnap < kMinSpan, "a span inside a unit is a piece");
