@@ -31,8 +31,8 @@ def regs(x):
     return [x]
 
 
-def run(lines, D, start, tiles):
-    """Interprets from label `start` on until `tiles` tiles are done; returns what registers hold and a trace."""
+def run(lines, D, start, tiles, held=()):
+    """Interprets from label `start` on until `tiles` tiles are done; returns what registers hold and a trace.  `held`: more registers at the start."""
     rowb, tile_bytes = 2 * D, gen.KT * 2 * D
     value, age, written_by = {}, {}, {}
     for (ks, qb), r in gen.Q.items():
@@ -44,6 +44,7 @@ def run(lines, D, start, tiles):
             for v in range(4):
                 value[f"v{r + v}"] = ("o", db, qb, ())
     value["%[l0]"], value["%[l1]"] = ("l", 0, ()), ("l", 1, ())
+    value.update(held)
     pending = []                                     # reads on their way: (registers, what)
     dma = 0
     clock = 0
@@ -223,3 +224,33 @@ def test_the_statement_says_what_it_writes(D, fp16):
     assert fixed <= said
     queries = {f"v{i}" for a, b in re.findall(r'"\{v\[(\d+):(\d+)\]\}"', rest) for i in range(int(a), int(b) + 1)}
     assert queries and not queries & (said | fixed)
+
+
+@pytest.mark.parametrize("second", [False, True])
+@pytest.mark.parametrize("D,fp16", STATEMENTS)
+def test_a_product_by_itself(D, fp16, second):
+    """S^T of all four blocks of keys, and O^T plus both halves' products."""
+    text = gen.one_product(D, fp16, second)
+    lines = ["s_begin:", *re.findall(r'"(.*?)\\n\\t"', text)]
+    assert lines[-2:] == ["s_nop 7", "s_nop 7"] and all(("_f16 v" in x) == fp16 for x in lines if "mfma" in x)
+    P = {f"v{gen.P[h, qb] + v}": ("weights", h, qb) for h in range(2) for qb in range(2) for v in range(4)}
+    value, _ = run([".Ldf_b0_%=:", *lines[1:]], D, ".Ldf_b0_%=", 1, P if second else ())
+    rowb = 2 * D
+    for qb in range(2):
+        if second:
+            for db in range(D // 16):
+                terms = tuple((tuple(("ds_read_b64_tr_b16", f"%[v{db}]", (32 * h + 4 * u) * rowb) for u in range(2)), (("weights", h, qb),)) for h in range(2))
+                for v in range(4):
+                    assert value[f"v{gen.O[db, qb] + v}"] == ("o", db, qb, terms)
+        else:
+            for kb in range(4):
+                terms = tuple(((("ds_read_b128", f"%[k{ks}]", (32 * (kb // 2) + 4 * (kb % 2)) * rowb),), (("q", ks, qb),)) for ks in range(D // 32))
+                for v in range(4):
+                    assert value[f"v{gen.S[kb, qb] + v}"][-1] == terms
+    # every register that is written is an output or said to be
+    said = {f"v{i}" for i in re.findall(r'"v(\d+)"', text)}
+    for a, b in re.findall(r'"(?:\+|=&)\{v\[(\d+):(\d+)\]\}"', text):
+        said |= {f"v{i}" for i in range(int(a), int(b) + 1)}
+    for x in lines:
+        m = re.match(r"(v_mfma\w+|ds_read\w+)\s+(v\[\d+:\d+\]),", x)
+        assert not m or set(regs(m[2])) <= said
