@@ -160,8 +160,7 @@ __device__ __forceinline__ Span my_span(const PagedParams &p, Entry *lds, int64_
   }
   const int wgs = gridDim.x;
   Span sp;
-  sp.line.all = uniform(all);
-  sp.line.count = __builtin_amdgcn_readfirstlane(span_count(all, wgs));
+  sp.line = Line::of(uniform(all), wgs);
   const int count = sp.line.count;
   // Workgroups are dealt to the eight XCDs in turn: with a full launch an XCD takes neighbouring spans, which read the same keys.
   sp.index = count == wgs && wgs % 8 == 0 ? int(blockIdx.x % 8) * (wgs / 8) + int(blockIdx.x / 8) : int(blockIdx.x);

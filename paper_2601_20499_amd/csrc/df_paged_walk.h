@@ -232,21 +232,32 @@ DF_WALK int cut_at(int64_t x, int T) {
 
 struct Line {
   int64_t all;               // its length
-  int count;                 // spans
+  int count;                 // spans: as many as there are workgroups, fewer on a line shorter than kMinSpan each
+  int64_t each;              // all = each * count + rest
+  int rest;
+  DF_WALK static Line of(int64_t all, int workgroups) {
+    const int64_t n = all / kMinSpan;
+    Line x{all, int(n < 1 ? (all > 0) : n > workgroups ? workgroups : n), 0, 0};
+    // (a division in 64 bits takes a wave half a microsecond)
+    if (x.count == 0) return x;
+    if ((x.count & (x.count - 1)) == 0) x.each = all >> __builtin_ctz(x.count);
+    else x.each = all <= UINT32_MAX ? unsigned(all) / unsigned(x.count) : all / x.count;
+    x.rest = int(all - x.each * x.count);
+    return x;
+  }
   // Where a span begins (of the one behind the last: the line's end).
-  DF_WALK int64_t begin_of(int i) const { return all * i / count; }
+  DF_WALK int64_t begin_of(int i) const {
+    const unsigned r = unsigned(rest) * unsigned(i), c = unsigned(count);
+    return each * i + ((c & (c - 1)) == 0 ? r >> __builtin_ctz(c) : r / c);
+  }
   // How far into its span position x lies.
   DF_WALK int64_t into_span(int64_t x) const {
-    int i = int(x * count / all);
+    int i = clamp_int(int(float(x) * (float(count) / float(all))), 0, count - 1);
     while (begin_of(i) > x) --i;
     while (begin_of(i + 1) <= x) ++i;
     return x - begin_of(i);
   }
 };
-DF_WALK int span_count(int64_t all, int workgroups) {
-  const int64_t n = all / kMinSpan;
-  return int(n < 1 ? (all > 0) : n > workgroups ? workgroups : n);
-}
 
 // A span's part of a unit of T tiles that begins at `at` on the line.
 struct Piece {
@@ -262,7 +273,8 @@ DF_WALK Piece piece_of(const Line &line, int64_t begin, int64_t end, int64_t at,
   x.ends = x.t1 == T;
   x.is = x.t0 < x.t1 || (T == 0 && begin <= at);
   if (turned && T > 0 && x.is) {
-    const int turn = int(line.into_span(at) % T);
+    const int64_t into = line.into_span(at);
+    const int turn = into <= INT32_MAX ? int(unsigned(into) % unsigned(T)) : int(into % T);
     x.t0 += turn;
     x.t1 += turn;
     if (x.t0 >= T) {

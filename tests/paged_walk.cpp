@@ -64,13 +64,14 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
     cost[u] = un.row0 >= r.n * l.G ? 0 : kUnitCost + tiles_of<KT>(r, row_range(r, rules, un.row0, ROWS), l.keys).count();
     at[u + 1] = at[u] + cost[u];
   }
-  Line line{at[units], span_count(at[units], workgroups)};
+  const Line line = Line::of(at[units], workgroups);
   CHECK((line.all > 0) == (line.count > 0) && line.count <= workgroups);
   // seen[u][tile]: times taken; owner: pieces of cut units in span order
   std::vector<std::vector<int>> seen(units);
   std::vector<int> tail(line.count, -1), head(line.count, 0), head_unit(line.count, -1), whole(units, 0);
   for (int sp = 0; sp < line.count; ++sp) {
     const int64_t begin = line.begin_of(sp), end = line.begin_of(sp + 1);
+    CHECK(begin == line.all * sp / line.count && end == line.all * (sp + 1) / line.count);
     CHECK(end > begin);
     for (int u = 0; u < units && at[u] < end; ++u) {
       if (at[u + 1] <= begin && !(at[u + 1] == at[u])) continue;
