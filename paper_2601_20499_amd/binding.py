@@ -594,6 +594,7 @@ def df_paged_attn(q, k_cur, v_cur, cache: PagedCache, cu_new, out, softmax_scale
         _like(lse_out, cache._f32, (H_q, total), cache.device, "lse_out")
     a.cu_new, a.lse_out = _ptr(cu_new), _ptr(lse_out)
     a.H_q, a.total_new, a.max_new, a.block, a.softmax_scale = H_q, total, total if max_new is None else max_new, block, softmax_scale
+    _want(workspace is None or (workspace.is_contiguous() and workspace.device == cache.device), "workspace: contiguous, on the cache's device")
     a.workspace = _ptr(workspace)
     a.workspace_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(lib.df_paged_attn(C.byref(a), _stream_handle(stream)), "df_paged_attn")

@@ -311,7 +311,8 @@ PyObject *paged_attn(PyObject *, PyObject *const *x, Py_ssize_t n) {
       return nullptr;
     if (x[8] == Py_None) a.max_new = a.total_new;
     const PagedOf p(x[3]);
-    if (!p.cache || !p.rows(q, a.H_q, a.q_stride_tok, a.q_stride_head) || !p.rows(out, a.H_q, a.o_stride_tok, a.o_stride_head) ||
+    const at::Tensor *ws = tensor(x[10]);
+    if (!p.cache || (ws && !(ws->is_contiguous() && ws->device() == p.device)) || !p.rows(q, a.H_q, a.q_stride_tok, a.q_stride_head) || !p.rows(out, a.H_q, a.o_stride_tok, a.o_stride_head) ||
         out->size(0) != a.total_new || !p.array(x[4], at::kInt, {int64_t(p.cache->B) + 1}, a.cu_new) ||
         (x[9] != Py_None && !p.array(x[9], at::kFloat, {a.H_q, a.total_new}, a.lse_out)))
       return nullptr;

@@ -271,12 +271,13 @@ extern "C" df_status df_page_map(const df_page_map_args *a, void *stream) {
   p.B = c->B; p.H = c->H_kv; p.n_pages = c->n_pages; p.max_pages = c->max_pages;
   p.page_log2 = log2_of(c->page_tokens);
   p.total = a->total_new;
-  const int64_t slots = int64_t(a->total_new) * c->H_kv;
+  const int64_t slots = int64_t(a->total_new) * c->H_kv, blocks = (slots + kSlotsPerBlock - 1) / kSlotsPerBlock;
+  if (blocks * kSlotThreads > UINT32_MAX) return DF_ERR_RANGE;             // before anything is launched
   p.fused = slots < kFusedSlots;
   hipLaunchKernelGGL(df_page_map_kernel, dim3(1), dim3(kMapThreads), 0, static_cast<hipStream_t>(stream), p);
   if (df_status s = launch_status()) return s;
   if (!p.fused) {
-    hipLaunchKernelGGL(df_slot_kernel, dim3(unsigned((slots + kSlotsPerBlock - 1) / kSlotsPerBlock)), dim3(kSlotThreads), 0,
+    hipLaunchKernelGGL(df_slot_kernel, dim3(unsigned(blocks)), dim3(kSlotThreads), 0,
                        static_cast<hipStream_t>(stream), p);
     return launch_status();
   }
@@ -304,7 +305,7 @@ extern "C" df_status df_paged_append(const df_paged_append_args *a, void *stream
   p.H = c->H_kv;
   p.n_vec = int64_t(a->total_new) * c->H_kv * (c->d / 8);
   const int64_t blocks = (p.n_vec + kPutThreads * kPutVecs - 1) / (kPutThreads * kPutVecs);
-  if (blocks > INT32_MAX) return DF_ERR_RANGE;
+  if (blocks * kPutThreads > UINT32_MAX) return DF_ERR_RANGE;              // a launch counts its threads in 32 bits
   const dim3 grid(unsigned(blocks), 2);
   if (c->d == 128)
     hipLaunchKernelGGL((df_put_kernel<16>), grid, dim3(kPutThreads), 0, static_cast<hipStream_t>(stream), p);

@@ -266,6 +266,17 @@ def test_pages_far_into_a_pool(df, kind):
         assert torch.equal(pool[-1, -1], want[0, 0]) and torch.equal(pool.view(-1, d)[(1 << 32) // (2 * d)], want[1, 0])
 
 
+@pytest.mark.parametrize("B,H,n,G", [(1700, 10, 1, 2), (110, 20, 40, 1)])
+def test_very_many_requests(df, B, H, n, G):
+    """More heads than a workgroup notes in LDS, and more units than it looks at in one go."""
+    lens = [(7 * i) % 21 for i in range(B)]
+    b = pu.Batch(B, lens, [n if i % 5 else n // 2 for i in range(B)], [(0, FULL)] * (H - 1) + [(2, 9)], G, 64, BF16)
+    rows = sorted(range(0, sum(b.new), 97))
+    out, lse = run(df, b, 1)
+    pu.check(out, lse, b.reference(1, rows), BF16, 64, "%d requests" % B, rows=rows)
+    assert not out.isnan().any() and not (out == 7.0).all(-1).any()
+
+
 # ---- all three together -----------------------------------------------------------------------------------------------------------
 
 class Loop:

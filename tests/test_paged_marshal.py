@@ -42,3 +42,16 @@ def test_a_scale_that_leaves_32_bits_is_refused():
     from tests import test_paged_abi as abi
     for scale, code in ((3e38, df.DF_ERR_RANGE), (2e38, df.DF_ERR_WORKSPACE)):
         assert abi._calls(df, abi._cache(df), softmax_scale=scale, workspace=None)[2]() == code
+
+
+def test_batches_of_more_rows_than_a_launch_has_threads_are_refused():
+    from tests import test_paged_abi as abi
+    wide = abi._cache(df, H_kv=64, cap_stride=0)
+    assert abi._calls(df, wide, total_new=1 << 30)[0]() == df.DF_ERR_RANGE and abi._calls(df, wide, total_new=1 << 28)[1]() == df.DF_ERR_RANGE
+
+
+def test_a_workspace_that_is_not_what_it_counts_is_refused():
+    b = batch()
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 26), torch.zeros(64, 64)[:, ::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            df.df_paged_attn(b.q, None, None, b.cache(df), b.cu, b.q, 0.125, workspace=ws)
