@@ -408,19 +408,19 @@ struct Feed {
 
 // ---- one tile of keys against a wave's rows -------------------------------------------------------------------------------------
 
-// What masks need to know of a wave's rows, worked out once a piece, in LDS.
+// What each of a wave's rows sees of the slots (0) and of the new tokens (1), worked out once a piece, in LDS.
 template <int ROWS>
 struct RowNotes {
-  int first[ROWS];           // first token of the row's causal block
-  int ring;                  // slots of the ring in front of its oldest token
+  Keys of[2][ROWS];
   __device__ __forceinline__ void fill(const PagedParams &p, const Request &r, int row0) {
     const int lane = threadIdx.x & 63;
-    if (lane < ROWS) first[lane] = p.rules.first_of(min(row0 + lane, r.n * p.G - 1));
-    if (lane == 0) ring = ring_start(r);
+    if (lane < ROWS) {
+      const int first = p.rules.first_of(min(row0 + lane, r.n * p.G - 1));
+      of[0][lane] = row_slots(r, first);
+      of[1][lane] = row_fresh(r, p.rules, first);
+    }
   }
-  __device__ __forceinline__ Sight sight(const PagedParams &p, const Request &r, int qb, bool is_new) const {
-    return Sight::behind(r, p.rules, first[16 * qb + (lane_here() & 15)], is_new);
-  }
+  __device__ __forceinline__ Keys row(int qb, bool is_new) const { return of[is_new][16 * qb + (lane_here() & 15)]; }
 };
 // The products of a tile of 64 keys and 32 rows, each as one asm statement (df_paged_tiles.inc; operands on their way from LDS as in the loop over
 // tiles): S^T from the lane's first K operand on, O^T from its first V^T operand on.
@@ -506,22 +506,26 @@ struct Rows {
     __builtin_amdgcn_sched_group_barrier(0x8, A * QB, 0);
   }
 
-  // Scores of keys that a row does not see, and of those before `from`, become minus infinity.  (Without a branch: with one per key, and all
-  // scores moved around each, a tile of it took 10 us.)
-  __device__ __forceinline__ static void hide(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, int k0, bool is_new, int from, f32x4 (&s)[KB][QB]) {
+  // Scores of keys that a row does not see, and of those before `from`, become minus infinity.  A lane's keys are runs of eight: three bounds make eight bits
+  // of them, and a bit takes two instructions.  (With a comparison of every key with every bound, 365 instructions, 390-token frames took 78 us where
+  // they take 69; with a branch per key, 112.)
+  __device__ __forceinline__ static void hide(const RowNotes<16 * QB> &notes, int k0, bool is_new, int from, f32x4 (&s)[KB][QB]) {
     const int g = lane_here() >> 4;
-    const Order order = Order::of(r, is_new, int(scalar(unsigned(notes.ring))));
-    Sight sight[QB];
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) sight[qb] = notes.sight(p, r, qb, is_new);
+    for (int qb = 0; qb < QB; ++qb) {
+      const Keys x = notes.row(qb, is_new);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+      for (int ts = 0; ts < KB / 2; ++ts) {
+        const int k = k0 + 32 * ts + 8 * g;
+        const unsigned bits = eight_keys(x, k) & ~below8(from - k);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int key = k0 + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + v, pos = order.position(key);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb][v] = ((key >= from) & sight[qb].sees(key, pos)) ? s[kb][qb][v] : -INFINITY;
+        for (int i = 0; i < 8; ++i) {
+          const unsigned seen = unsigned(int(bits << (31 - i)) >> 31);
+          const float y = s[2 * ts + i / 4][qb][i % 4];  // (a bit_cast of an element itself takes the first one's bits)
+          s[2 * ts + i / 4][qb][i % 4] = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned, y) & seen) | (0xff800000u & ~seen));
+        }
       }
+    }
   }
 
   // Weights 2^(c s - c m) of row block qb, packed as the second product's operand, and their sum over the lane's keys.
@@ -574,12 +578,12 @@ struct Rows {
   // lane's weights add up to more than 2^15 (fp16 holds weights to 2^16, and sums and outputs stay far from the largest number
   // in 32 bits), and where a row has no reference yet, the wave looks for the maximum, brings what it has to the new reference
   // and weighs the tile again.  That leaves the common tile without a maximum, a comparison per score or a product of the outputs.
-  __device__ __forceinline__ void tile(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, unsigned k, unsigned v, int k0, bool is_new, int from, int seen) {
+  __device__ __forceinline__ void tile(const PagedParams &p, const RowNotes<16 * QB> &notes, unsigned k, unsigned v, int k0, bool is_new, int from, int seen) {
     f32x4 s[KB][QB];
     s16x8 w[KB / 2][QB];
     float sum[QB];
     scores(k, s);
-    if (__builtin_expect(seen != kAllSeen, 0)) hide(p, r, notes, k0, is_new, from, s);
+    if (__builtin_expect(seen != kAllSeen, 0)) hide(notes, k0, is_new, from, s);
     constexpr bool kAsm = KB == 4 && QB == 2;
     Values x;
     if constexpr (!kAsm) x = begin_values(v);
@@ -596,7 +600,7 @@ struct Rows {
     }
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) l[qb] += sum[qb];
-    if (__builtin_expect(seen == kSomeHidden && odd_values(v), 0)) odd_products(p, r, notes, v, k0, is_new, w);
+    if (__builtin_expect(seen == kSomeHidden && odd_values(v), 0)) odd_products(notes, v, k0, is_new, w);
     else if constexpr (kAsm) values_of<T, D>(v_first(v), w, o);
     else values(x, w);
   }
@@ -643,17 +647,19 @@ struct Rows {
   // its key: what an infinity or a NaN times a weight adds.
   __device__ __forceinline__ static bool odd_values(unsigned v) {
     typedef u16 u16x8 __attribute__((ext_vector_type(8)));
-    const unsigned first = v_first(v);
+    const unsigned first = v + 16u * unsigned(lane_here());
     u16x8 top = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kValueOps; ++i)
-      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x8, v_operand(first, i / DB, i % DB)) & u16(0x7fff));
+    for (int i = 0; i < 16 * KB * Layout<D>::ROWB / 1024; ++i) {
+      const s16x8 x = *(const lds_s16x8 *)(uintptr_t)(first + 1024 * i);
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x8, x) & u16(0x7fff));
+    }
     u16 most = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) most = most > top[k] ? most : top[k];
     return __builtin_amdgcn_ballot_w64(most >= T::kExponent) != 0;
   }
-  __device__ __forceinline__ void odd_products(const PagedParams &p, const Request &r, const RowNotes<16 * QB> &notes, unsigned v, int k0, bool is_new, const s16x8 (&w)[KB / 2][QB]) {
+  __device__ __forceinline__ void odd_products(const RowNotes<16 * QB> &notes, unsigned v, int k0, bool is_new, const s16x8 (&w)[KB / 2][QB]) {
     using L = Layout<D>;
     const unsigned first = v_first(v);
 #pragma unroll
@@ -665,13 +671,11 @@ struct Rows {
       for (int qb = 0; qb < QB; ++qb) o[i % DB][qb] = T::mfma(a, w[i / DB][qb], o[i % DB][qb]);
     }
     const int g = lane_here() >> 4;
-    const Order order = Order::of(r, is_new, int(scalar(unsigned(notes.ring))));
-    Sight sight[QB];
+    Keys row_sees[QB];
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) sight[qb] = notes.sight(p, r, qb, is_new);
+    for (int qb = 0; qb < QB; ++qb) row_sees[qb] = notes.row(qb, is_new);
 #pragma unroll 1
     for (int key = 0; key < 16 * KB; ++key) {
-      const int pos = order.position(k0 + key);
       const unsigned row = v + unsigned(key * L::ROWB);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
@@ -682,7 +686,7 @@ struct Rows {
           const bool odd = (u16(x[i]) & T::kExponent) == T::kExponent;
           const float f = odd ? ((u16(x[i]) & ~(T::kExponent | 0x8000u)) ? NAN : (u16(x[i]) & 0x8000u) ? -INFINITY : INFINITY) : 0.f;
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) o[db][qb][i] += sight[qb].sees(k0 + key, pos) ? f : 0.f;
+          for (int qb = 0; qb < QB; ++qb) o[db][qb][i] += row_sees[qb].sees(k0 + key) ? f : 0.f;
         }
       }
     }
@@ -819,7 +823,7 @@ __global__ __launch_bounds__(kThreads, 2) void df_paged_many_kernel(const PagedP
           if (t + 1 < t1) next = ld.bring(other, other + TILE);
         }
         if (now.seen != kNoneSeen)
-          rows.tile(p, r, notes[wave], buf, buf + TILE, now.k0, now.is_new, due == 2 ? now.k0 + KT / 2 : now.k0, due == 2 ? int(kSomeHidden) : now.seen);
+          rows.tile(p, notes[wave], buf, buf + TILE, now.k0, now.is_new, due == 2 ? now.k0 + KT / 2 : now.k0, due == 2 ? int(kSomeHidden) : now.seen);
         now = next;
         buf = other;
       }
@@ -910,7 +914,7 @@ __global__ __launch_bounds__(kThreads) void df_paged_few_kernel(const PagedParam
         // this tile has landed, the next one may still be on its way
         if (t + kFewWaves < t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (now.seen != kNoneSeen) rows.tile(p, r, notes[wave], buf, buf + TILE, now.k0, now.is_new, now.k0, now.seen);
+        if (now.seen != kNoneSeen) rows.tile(p, notes[wave], buf, buf + TILE, now.k0, now.is_new, now.k0, now.seen);
         now = next;
         if (t + 2 * kFewWaves < t1) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the reads of this buffer are done

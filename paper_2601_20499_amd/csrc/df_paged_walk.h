@@ -153,7 +153,10 @@ DF_WALK Place place_of(const Request &r, const Tiles<KT> &tl, int t) {
 }
 
 // Keys that the rows of a range see of the cache (`hist`) and of the new tokens (`fresh`): [0, a) and [b, c), `all` of them or `some`.
-struct Keys { int a, b, c; };
+struct Keys {
+  int a, b, c;
+  DF_WALK bool sees(int key) const { return (key < a) | ((key >= b) & (key < c)); }
+};
 DF_WALK Keys pick(bool first, const Keys &x, const Keys &y) { return Keys{pick(first, x.a, y.a), pick(first, x.b, y.b), pick(first, x.c, y.c)}; }
 struct RangeKeys {
   Keys all_hist, all_fresh, some_hist, some_fresh;
@@ -177,34 +180,18 @@ DF_WALK Seen seen_of(const Place &x, int KT, const RangeKeys &k) {
   return x.k0 + KT <= until ? kAllSeen : least(x.k0 + KT, x.limit) <= until ? kTailMissing : kSomeHidden;
 }
 
-// What one row sees of keys.
-struct Sight {
-  int lim, end;              // lowest position, and key behind the last one
-  // Of a row whose causal block begins at token `first`.
-  DF_WALK static Sight behind(const Request &r, const Rules &u, int first, bool is_new) {
-    const int end = int(u.block.d) < r.n ? least(first + int(u.block.d), r.n) : r.n;
-    return Sight{(is_new ? 0 : r.L) + first - r.w, pick(is_new, end, r.held)};
-  }
-  DF_WALK bool sees(int key, int pos) const { return (key < end) & (pos >= lim); }       // (no branch)
-};
-// Slots of the ring in front of its oldest token, -1 if it is not full.
-DF_WALK int ring_start(const Request &r) {
-  const int turn = r.L - r.s;
-  return turn > r.w && r.w > 0 ? turn % r.w : -1;
+// What one row sees, whose causal block begins at token `first`: slots, and new tokens.
+DF_WALK Keys row_slots(const Request &r, int first) {
+  const Visible v = visible_slots(r, first);
+  return Keys{v.a1, v.b0, v.b1};
 }
-// Positions of keys in a form without branches: the largest number (windows do not matter) below key `a`, key + c below key `b`, key + d from there on.
-struct Order {
-  int a, b, c, d;
-  DF_WALK static Order of(const Request &r, bool is_new, int ring) {
-    const bool turned = !is_new && ring >= 0;
-    const int c = turned ? r.L - ring - r.s : 0;
-    return Order{is_new ? r.s - r.L : r.s, turned ? r.s + ring : INT32_MAX, c, turned ? c - r.w : 0};
-  }
-  DF_WALK int position(int key) const {
-    const int at = key + (key < b ? c : d);
-    return key < a ? INT32_MAX : at;
-  }
-};
+DF_WALK Keys row_fresh(const Request &r, const Rules &u, int first) {
+  const int end = int(u.block.d) < r.n ? least(first + int(u.block.d), r.n) : r.n;
+  return Keys{clamp_int(r.s - r.L, 0, end), most(0, first - r.w), end};
+}
+// Which of the keys k .. k + 7 they are: a bit for each.
+DF_WALK unsigned below8(int n) { return (1u << clamp_int(n, 0, 8)) - 1u; }
+DF_WALK unsigned eight_keys(const Keys &x, int k) { return below8(x.a - k) | (below8(x.c - k) & ~below8(x.b - k)); }
 
 // ---- sharing out -------------------------------------------------------------------------------------------------------------
 // The units' costs (tiles + a constant) form a line, requests outermost, then key heads, then tiles of rows (neighbours read the same keys); it is

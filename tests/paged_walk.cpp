@@ -95,7 +95,6 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
         CHECK(pl.k0 % KT == 0 && pl.k0 >= 0 && pl.k0 < pl.limit);
       }
       // waves: what is taken as seen by all is, of what is skipped nothing is, and where only the tail is missing all that is there is seen
-      const int ring = ring_start(r);
       for (int wave = 0; wave < WAVES; ++wave) {
         const int rows = ROWS / WAVES, row0 = un.row0 + rows * wave, last = r.n * l.G;
         if (row0 >= last) continue;
@@ -105,11 +104,10 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
           const Place pl = place_of(r, tl, t);
           const Seen what = seen_of(pl, KT, rk);
           if (what == kSomeHidden) continue;
-          const Order order = Order::of(r, pl.is_new, ring);
           for (int row = row0; row < least(row0 + rows, last); ++row) {
-            const Sight s = Sight::behind(r, rules, rules.first_of(row), pl.is_new);
+            const Keys s = pl.is_new ? row_fresh(r, rules, rules.first_of(row)) : row_slots(r, rules.first_of(row));
             for (int k = pl.k0; k < pl.k0 + KT; ++k)
-              CHECK(s.sees(k, order.position(k)) == (what == kAllSeen || (what == kTailMissing && k < pl.limit)));
+              CHECK(s.sees(k) == (what == kAllSeen || (what == kTailMissing && k < pl.limit)));
           }
         }
       }
@@ -134,7 +132,7 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
     const Unit un = unit_of(u, by_tiles, by_heads, ROWS);
     const Request r = request(un.b, un.h);
     const Tiles<KT> tl = tiles_of<KT>(r, row_range(r, rules, un.row0, ROWS), l.keys);
-    const int T = tl.count(), ring = ring_start(r), n = l.cu[un.b + 1] - l.cu[un.b], L = l.len[un.b], s = r.s, w = r.w;
+    const int T = tl.count(), n = l.cu[un.b + 1] - l.cu[un.b], L = l.len[un.b], s = r.s, w = r.w;
     std::vector<char> slot_in(r.held, 0), new_in(n, 0);
     for (int t = 0; t < T; ++t) {
       const Place pl = place_of(r, tl, t);
@@ -146,7 +144,13 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
     for (int row = un.row0; row < least(un.row0 + ROWS, n * l.G); row += pick(1, 9)) {
       const int i = row / l.G, first = int(int64_t(i) / l.block * l.block);
       const int64_t last = int64_t(first) + l.block < n ? int64_t(first) + l.block : n;
-      const Sight hist = Sight::behind(r, rules, rules.first_of(row), false), fresh = Sight::behind(r, rules, rules.first_of(row), true);
+      const Keys hist = row_slots(r, rules.first_of(row)), fresh = row_fresh(r, rules, rules.first_of(row));
+      for (const Keys &x : {hist, fresh})
+        for (int k = 0; k < most(r.held, n) + 8; k += 8) {
+          unsigned bits = 0;
+          for (int i = 0; i < 8; ++i) bits |= unsigned(x.sees(k + i)) << i;
+          CHECK(eight_keys(x, k) == bits);
+        }
       int held = 0;
       for (int j = 0; j < L; ++j) {
         if (!(j < s || (w > 0 && j >= L - w))) continue;    // not kept
@@ -154,14 +158,14 @@ static void walk(const Launch &l, int seed, int workgroups, bool turned) {
         const int slot = slot_of(j, s, w);
         CHECK(slot < r.held);
         const bool sees = j < s || j >= L + first - w;
-        CHECK(hist.sees(slot, Order::of(r, false, ring).position(slot)) == sees);
+        CHECK(hist.sees(slot) == sees);
         if (sees) CHECK(slot_in[slot] == 1);
       }
       CHECK(held == r.held);
-      for (int k = r.held; k < r.held + KT; ++k) CHECK(!hist.sees(k, Order::of(r, false, ring).position(k)));
+      for (int k = r.held; k < r.held + KT; ++k) CHECK(!hist.sees(k));
       for (int t = 0; t < n + KT; ++t) {
         const bool sees = t < last && (t >= first - w || L + t < s);
-        CHECK(fresh.sees(t, Order::of(r, true, ring).position(t)) == sees);
+        CHECK(fresh.sees(t) == sees);
         if (sees && l.keys) CHECK(new_in[t] == 1);
       }
     }
