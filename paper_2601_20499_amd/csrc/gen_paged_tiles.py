@@ -103,7 +103,7 @@ def tile(D, mfma, pack, buf):
             for k, r in enumerate(ops[i][1]):
                 lines.append(r.replace("@", f"v[{slot(i) + w * k}:{slot(i) + w * k + w - 1}]"))
 
-    beside = {1: half_softmax(0, pack), 2: half_softmax(1, pack)}
+    beside = {0: bring(D, buf), 1: half_softmax(0, pack), 2: half_softmax(1, pack)}
     for i in range(DEPTH):
         issue(i)
     for phase in range(4):
@@ -159,7 +159,6 @@ def statement(D, fp16):
     for buf in range(2):
         lines.append(f".Ldf_b{buf}_%=:")
         lines += ["s_waitcnt vmcnt(0)", "s_barrier"]
-        lines += bring(D, buf)
         lines += tile(D, mfma, pack, buf)
         lines += ["s_sub_i32 %[n], %[n], 1", "s_cmp_eq_u32 %[n], 0"]
         lines += ["s_cbranch_scc1 .Ldf_end_%="] if buf == 0 else ["s_cbranch_scc0 .Ldf_b0_%=", "s_branch .Ldf_end_%="]
