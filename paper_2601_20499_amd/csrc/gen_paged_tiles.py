@@ -11,7 +11,10 @@ A tile is 64 keys in two halves h of 32.  A wave's 32 rows go through it in four
 
 The vector instructions of a half lie between the products of the other half, so that a wave by itself keeps both units busy for half
 of its time; the other wave of the SIMD, of another workgroup and at another place of its tile, fills the rest.  Operands come from LDS
-with DEPTH of them in flight, each waited for by count.  Before the products of a half its sums are looked at: where one is over
+with DEPTH of them in flight, each waited for by count.  The next tile's loads are issued between the products of S(0).  The wave's priority
+follows the phases, so that the two waves of a SIMD move apart and stay apart: the one nearest the end of its vector work goes first, the one in
+the last phase, which only the matrix core holds up, goes last.  1280x720 chunk, priorities by phase: all equal 2550 us, 1 1 1 0 2455, 0 0 1 0 2348,
+1 1 2 0 2295; 1 0 0 1 2570.  Before the products of a half its sums are looked at: where one is over
 32768, or is no number, the statement ends, O as it was before that half, and the caller takes the rest of the tile another way.
 
 Why asm: written in C++ the compiler read most operands right before their use (a wait of 64 to 128 cycles each), and took 250 vector
@@ -41,6 +44,7 @@ Q = {(ks, qb): Q0 + 8 * ks + 4 * qb for ks in range(4) for qb in range(2)}
 O0 = Q0 - 64
 O = {(db, qb): O0 + 8 * db + 4 * qb for db in range(8) for qb in range(2)}
 TMP = O0 - 12                                    # three groups of four exponentials
+PRIORITY = (1, 1, 2, 0)                          # of the wave, by phase
 DK, DV = 64, 68                                  # descriptors
 
 
@@ -108,6 +112,7 @@ def tile(D, mfma, pack, buf):
         issue(i)
     for phase in range(4):
         mine = [i for i, o in enumerate(ops) if o[0] == phase]
+        lines.append(f"s_setprio {PRIORITY[phase]}")
         vector = list(beside.get(phase, []))
         # the first vector instruction of a phase reads what the last products of the phase before have written
         skip = 3 if phase == 1 else 0
@@ -163,7 +168,7 @@ def statement(D, fp16):
         lines += ["s_sub_i32 %[n], %[n], 1", "s_cmp_eq_u32 %[n], 0"]
         lines += ["s_cbranch_scc1 .Ldf_end_%="] if buf == 0 else ["s_cbranch_scc0 .Ldf_b0_%=", "s_branch .Ldf_end_%="]
     lines += [".Ldf_over1_%=:", "s_mov_b32 %[due], 1", ".Ldf_over0_%=:", "s_add_i32 %[due], %[due], 1", "s_waitcnt lgkmcnt(0)",
-              ".Ldf_end_%=:", "s_nop 7", "s_nop 7"]
+              ".Ldf_end_%=:", "s_setprio 0", "s_nop 7", "s_nop 7"]
     KS, DB, loads = D // 32, D // 16, D // 32
     outs = [f'"+{{{quad(O[db, qb])}}}"(o[{db}][{qb}])' for db in range(DB) for qb in range(2)]
     outs += [f'[l{qb}] "+v"(l[{qb}])' for qb in range(2)]

@@ -90,7 +90,7 @@ def run(lines, D, start, tiles, held=()):
         if op == "s_barrier":
             assert dma == 0 and not pending, "all reads and loads are waited for before the barrier"
             trace["barriers"] += 1
-        elif op in ("s_nop", "s_mov_b32", "s_add_i32", "s_mul_hi_u32", "s_mul_i32", "s_addc_u32", "v_readlane_b32", "s_sub_i32", "s_cmp_eq_u32"):
+        elif op in ("s_nop", "s_mov_b32", "s_add_i32", "s_mul_hi_u32", "s_mul_i32", "s_addc_u32", "v_readlane_b32", "s_sub_i32", "s_cmp_eq_u32", "s_setprio"):
             if op == "s_sub_i32":
                 n -= 1
         elif op == "s_add_u32":
@@ -222,6 +222,8 @@ def test_the_statement_says_what_it_writes(D, fp16):
         said |= {f"v{i}" for i in range(int(a), int(b) + 1)}
     fixed = {r for r in written if r.startswith("v")}
     assert fixed <= said
+    # whatever way the statement ends, the wave's priority is the ordinary one again
+    assert re.findall(r'"(.*?)\\n\\t"', body)[-4:] == [".Ldf_end_%=:", "s_setprio 0", "s_nop 7", "s_nop 7"]
     queries = {f"v{i}" for a, b in re.findall(r'"\{v\[(\d+):(\d+)\]\}"', rest) for i in range(int(a), int(b) + 1)}
     assert queries and not queries & (said | fixed)
 
