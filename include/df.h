@@ -6,15 +6,17 @@
  * attends to its own slice of history (sink frames, a recent window, or
  * nothing) followed by the keys of the current chunk.  It also scores heads by
  * where their attention mass falls, classifies them, and maintains the
- * per-head sliding-window cache.
+ * per-head sliding-window cache.  For batches of requests whose lengths lie on
+ * the device there is a paged form of the cache with its own attention call.
  *
  * Conventions
  *   - "DEVICE" pointers address GPU memory of the current HIP device; "HOST"
  *     pointers address ordinary process memory.  The library never allocates or
  *     frees device memory and keeps no state between calls: the caller owns
  *     every buffer, including the workspace.
- *   - Tensors are bf16 (IEEE bfloat16 bit patterns) with the head dimension d
- *     contiguous.  Strides are given in elements.  d is 64 or 128.
+ *   - Tensors are bf16 (IEEE bfloat16 bit patterns), in the paged cache's calls
+ *     bf16 or fp16, with the head dimension d contiguous.  Strides are given in
+ *     elements.  d is 64 or 128.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     Device work is enqueued asynchronously; host arrays passed to a call
  *     are read (and, where stated, written) before the call returns.
