@@ -4,8 +4,9 @@
 // df_page_map.  need(b, h) = pages after the step - pages before it; an exclusive sum over (request, head) says which
 // free pages a head takes.  Latency bounds it: a few KB are read, and the sum, the check of the whole step (all or
 // nothing) and the writes depend on each other, so one workgroup does all of it between barriers, and no other
-// workgroup or launch has to agree on anything.  Only the slot map (8 bytes per token and head) can be large; from
-// kFusedSlots entries on a second kernel writes it with the whole device, below that the same workgroup does.
+// workgroup or launch has to agree on anything (64 requests of 8 heads: 6.3 us, of which an empty launch is 2.4).
+// Only the slot map (8 bytes per token and head) can be large; from kFusedSlots entries on a second kernel writes it
+// with the whole device, below that the same workgroup does.
 //
 // df_paged_append.  A row mover like df_rows_kernel, bound by HBM; destinations come from the slot map.
 #include "df_paged.h"
@@ -15,6 +16,7 @@ namespace df {
 constexpr int kMapThreads = 1024;
 constexpr int kMapWaves = kMapThreads / 64;
 constexpr int kFusedSlots = 8192;
+constexpr int kCuInLds = 4096;           // requests whose offsets are bisected in LDS
 
 struct MapParams {
   int *table;
@@ -107,8 +109,11 @@ __device__ __forceinline__ int64_t slot_for(const MapParams &p, const Cu &cu, in
 __global__ __launch_bounds__(kMapThreads) void df_page_map_kernel(const MapParams p) {
   __shared__ int64_t wave_sums[kMapWaves];
   __shared__ int line[kMapThreads + 1], first_new[kMapThreads];
-  __shared__ int bad_flag;
+  __shared__ int bad_flag, cu_lds[kCuInLds + 1];
   const int tid = threadIdx.x, E = p.B * p.H;
+  const bool in_lds = p.fused && p.B <= kCuInLds;        // (read below, behind barriers)
+  if (in_lds)
+    for (int b = tid; b <= p.B; b += kMapThreads) cu_lds[b] = p.cu[b];
   const int have = *p.n_free;
   if (tid == 0) bad_flag = 0;
   bool bad = have < 0 || have > p.n_pages || p.cu[0] < 0;
@@ -120,9 +125,9 @@ __global__ __launch_bounds__(kMapThreads) void df_page_map_kernel(const MapParam
     need += mine.after > mine.before ? mine.after - mine.before : 0;
     back += mine.released;
   }
-  int64_t need_all, back_all;
-  exclusive_sum(need, wave_sums, need_all);
-  exclusive_sum(back, wave_sums, back_all);
+  int64_t need_all, back_all = 0;
+  const int64_t need_before = exclusive_sum(need, wave_sums, need_all);
+  if (p.release) exclusive_sum(back, wave_sums, back_all);
   bad |= need_all > have + back_all || have + back_all > p.n_pages;
   // what is taken from the stack as it is has to be pages
   if (!bad)
@@ -140,9 +145,9 @@ __global__ __launch_bounds__(kMapThreads) void df_page_map_kernel(const MapParam
       const int e = e0 + tid;
       HeadPages hp{0, 0, 0, false};
       if (e < E) hp = E <= kMapThreads ? mine : head_pages(p, e);
-      int64_t count;
+      int64_t count = need_all;
       const int n = pass != kTake ? hp.released : hp.after > hp.before ? hp.after - hp.before : 0;
-      line[tid] = int(exclusive_sum(n, wave_sums, count));
+      line[tid] = int(pass == kTake && E <= kMapThreads ? need_before : exclusive_sum(n, wave_sums, count));
       first_new[tid] = hp.before;
       if (tid == 0) line[kMapThreads] = int(count);
       __syncthreads();
@@ -182,13 +187,12 @@ __global__ __launch_bounds__(kMapThreads) void df_page_map_kernel(const MapParam
   __syncthreads();
   for (int i = tid; i < p.total * p.H; i += kMapThreads) {
     const int t = i / p.H, h = i - t * p.H;
-    p.slots[i] = ok ? slot_for(p, p.cu, t, h, true) : -1;
+    p.slots[i] = !ok ? -1 : in_lds ? slot_for(p, cu_lds, t, h, true) : slot_for(p, p.cu, t, h, true);
   }
 }
 
 constexpr int kSlotThreads = 256;
 constexpr int kSlotsPerBlock = 1024;
-constexpr int kCuInLds = 4096;           // requests whose offsets are bisected in LDS
 
 __global__ __launch_bounds__(kSlotThreads) void df_slot_kernel(const MapParams p) {
   __shared__ int cu_lds[kCuInLds + 1];
