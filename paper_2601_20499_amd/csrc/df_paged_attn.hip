@@ -315,7 +315,7 @@ struct Feed {
   int t, lane;               // the tile that is brought next, and its lane
   unsigned slots[GROUPS];    // per lane: first row of the tile's group, among the head's pages or the request's new tokens
   int keys;                  // per lane: the tile's first key
-  uint64_t there, fresh, whole, seen1, seen2;            // tiles that exist, of new tokens, with all rows, and what is seen of them (two bits)
+  uint64_t fresh, whole, seen1, seen2;                   // tiles of new tokens, with all rows, and what is seen of them (two bits)
   bool bad;                  // per lane: a page was no page of the pool
 
   __device__ __forceinline__ Feed(const PagedParams &p_, const Request &r_, const Tiles<KT> &tl_, const RangeKeys &seen_, bool live_, int b, int h, int grp0_,
@@ -330,7 +330,6 @@ struct Feed {
     const bool is = mine < end;
     const int what = live ? int(seen_of(x, KT, seen)) : int(kNoneSeen);
     keys = x.k0;
-    there = __builtin_amdgcn_ballot_w64(is);
     fresh = __builtin_amdgcn_ballot_w64(x.is_new);
     whole = __builtin_amdgcn_ballot_w64(is && x.k0 + KT <= x.limit);
     seen1 = __builtin_amdgcn_ballot_w64(what & 1);

@@ -413,6 +413,64 @@ def test_a_step_on_another_stream(df):
         loop.agrees(slots, loop.advance(k, v, new))
 
 
+def test_two_calls_at_once(df):
+    """Calls on two streams, each with a workspace of its own, and two captured ones replayed beside each other: as one after the other."""
+    calls = []
+    for seed, (lens, new, G, block) in enumerate([([4000, 900], [1, 1], 4, 1), ([700, 0, 1200], [130, 64, 1], 1, 40)]):
+        b = pu.Batch(20 + seed, lens, new, [(0, FULL), (8, 300)], G, 128, BF16)
+        want, lse = run(df, b, block)
+        q, k, v = b.q.to(DEV), b.k_new.to(DEV), b.v_new.to(DEV)
+        ws = torch.empty(df.df_paged_workspace_bytes(2 * G, 2, 128, max(new)), dtype=torch.uint8, device=DEV)
+        out, ls, cache, stream = torch.empty_like(want), torch.empty_like(lse), b.cache(df), torch.cuda.Stream()
+        call = lambda b=b, q=q, k=k, v=v, ws=ws, out=out, ls=ls, cache=cache, block=block, new=new: df.df_paged_attn(
+            q, k, v, cache, b.cu, out, b.scale, block=block, max_new=max(new), lse_out=ls, workspace=ws)
+        calls.append((call, stream, out, ls, want, lse))
+    torch.cuda.synchronize()
+
+    def same():
+        torch.cuda.synchronize()
+        for _, _, out, ls, want, lse in calls:
+            assert torch.equal(out, want) and torch.equal(ls, lse)
+            out.fill_(7.0)
+            ls.fill_(7.0)
+        torch.cuda.synchronize()
+    for _ in range(5):
+        for call, stream, *_ in calls:
+            with torch.cuda.stream(stream):
+                call()
+    same()
+    graphs = []
+    for call, stream, *_ in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            call()
+        graphs.append(g)
+    same_first = [c[2].clone() for c in calls]
+    assert all((x == 7.0).all() for x in same_first)        # captured, not run
+    for _ in range(3):
+        for g, (_, stream, *_rest) in zip(graphs, calls):
+            with torch.cuda.stream(stream):
+                g.replay()
+        same()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_batches_of_nothing(df, kind):
+    """No request has a new token: nothing is written, and the map changes nothing."""
+    n, G, block = KINDS[kind]
+    b = pu.Batch(16, [60, 5], [n, n], [(0, FULL)], G, 64, BF16)
+    for at in (0, 3, 2 * n):
+        b.cu = ints([at] * 3)
+        out, lse = run(df, b, block)
+        assert (out == 7.0).all() and (lse == 7.0).all()
+        slots, status = torch.zeros(2 * n, 1, dtype=torch.int64, device=DEV), ints([5])
+        before = [x.clone() for x in (b.table, b.length, b.free, b.n_free)]
+        df.df_page_map(b.cache(df), b.cu, slots, status)
+        torch.cuda.synchronize()
+        assert status.item() == df.DF_OK and (slots == -1).all()
+        assert all(torch.equal(x, y) for x, y in zip(before, (b.table, b.length, b.free, b.n_free)))
+
+
 def test_one_request_is_the_dense_call(df):
     """A single request whose new tokens all see each other: what df_attn_fwd computes from packed histories."""
     caps = [(0, FULL), (20, 60), (0, 40), (0, 0)]
