@@ -151,7 +151,7 @@ def bring(D, buf):
     for which, d in (("k", DK), ("v", DV)):
         for n in range(loads):
             off = to + (tile_bytes if which == "v" else 0) + 1024 * n
-            lines += [f"s_add_u32 m0, %[to], {off}", "s_nop 0", f"buffer_load_dwordx4 %[{which}o{n}], s[{d}:{d + 3}], 0 offen lds"]
+            lines += [f"s_add_u32 m0, %[to], {off:#x}", "s_nop 0", f"buffer_load_dwordx4 %[{which}o{n}], s[{d}:{d + 3}], 0 offen lds"]
     return lines
 
 

@@ -96,7 +96,7 @@ def run(lines, D, start, tiles, held=()):
         elif op == "s_add_u32":
             if args[0] == "m0":
                 assert args[1] == "%[to]"
-                m0, m0_at = int(args[2]), clock
+                m0, m0_at = int(args[2], 0), clock
         elif op == "buffer_load_dwordx4":
             assert clock - m0_at >= 2, "an instruction between m0 and the load"
             which = args[0][2]
