@@ -354,7 +354,7 @@ typedef struct df_page_map_args {
   int32_t *len_out;            /* DEVICE out [B]                                   */
   int32_t *n_free_out;         /* DEVICE out [1]                                   */
   int32_t *status;             /* DEVICE out [1]                                   */
-  int32_t total_new;           /* rows of slot_map (>= 0; 0: releases only)        */
+  int32_t total_new;           /* rows of slot_map (>= 0; 0: releases only); times H_kv at most 2^34 */
 } df_page_map_args;
 
 df_status df_page_map(const df_page_map_args *args, void *stream);
@@ -367,7 +367,7 @@ typedef struct df_paged_append_args {
   const void *v_new;
   int64_t stride_tok, stride_head;
   const int64_t *slot_map;     /* DEVICE [total_new, H_kv] */
-  int32_t total_new;
+  int32_t total_new;           /* times H_kv * d at most 2^36 */
 } df_paged_append_args;
 
 df_status df_paged_append(const df_paged_append_args *args, void *stream);
@@ -398,7 +398,7 @@ typedef struct df_paged_attn_args {
   int32_t H_q, total_new;      /* query heads (a multiple of H_kv, at most 64 times as many), rows of q     */
   int32_t max_new;             /* 1 <= . <= total_new, at least every n_b: a request's tokens beyond it are left out */
   int32_t block;               /* tokens of a causal block, > 0                                             */
-  float softmax_scale;         /* positive and finite                                                       */
+  float softmax_scale;         /* positive, times log2(e) still finite                                      */
   void *workspace; size_t workspace_bytes; /* DEVICE, >= df_paged_workspace_bytes(...), 256-byte aligned; scratch */
 } df_paged_attn_args;
 
