@@ -11,7 +11,8 @@ A tile is 64 keys in two halves h of 32.  A wave's 32 rows go through it in four
 
 The vector instructions of a half lie between the products of the other half, so that a wave by itself keeps both units busy for half
 of its time; the other wave of the SIMD, of another workgroup and at another place of its tile, fills the rest.  Operands come from LDS
-with DEPTH of them in flight, each waited for by count.  The next tile's loads are issued between the products of S(0).  The wave's priority
+with DEPTH of them in flight, each waited for by count (6 take eight registers more, which
+the code around the loop is short of: prompt pieces 456 us, 443 with 4, 443 with 3).  The next tile's loads are issued between the products of S(0).  The wave's priority
 follows the phases, so that the two waves of a SIMD move apart and stay apart: the one nearest the end of its vector work goes first, the one in
 the last phase, which only the matrix core holds up, goes last.  1280x720 chunk, priorities by phase: all equal 2550 us, 1 1 1 0 2455, 0 0 1 0 2348,
 1 1 2 0 2295; 1 0 0 1 2570.  Before the products of a half its sums are looked at: where one is over
@@ -35,7 +36,7 @@ checks that it is what this script writes.
 import os
 
 KT = 64
-DEPTH = 6
+DEPTH = 4
 STAGE = 256 - 4 * DEPTH
 P = {(h, qb): STAGE - 16 + 8 * h + 4 * qb for h in range(2) for qb in range(2)}
 S = {(kb, qb): STAGE - 48 + 8 * kb + 4 * qb for kb in range(4) for qb in range(2)}
