@@ -19,8 +19,8 @@
 // tiles at about the same time: a workgroup of the second kernel that comes to a unit t tiles after its start begins it at tile t (modulo
 // their number) and goes round, and where its span ends within the unit the next workgroup does the rest of the round.  All of them start
 // at the same tile, so at any time two places are read, by the workgroups on their first unit and by those past it.  1280x720 chunk: 21 GB
-// fetched past the L2s without this, 2.8 GB with it, and 2990 -> 2620 us.  Keys that fit are better read from the first to the last
-// (fewer runs of tiles: 390-token frames 85 us, 89 with turned rounds).
+// fetched past the L2s without this, 1.4 GB with it; 2990 -> 2620 us when it came (2230 to 2340 since).  Keys that fit are better read from the first to the last
+// (fewer runs of tiles: 390-token frames took 85 us, 89 with turned rounds, before they came down to 68).
 //
 // Lengths are on the device, so the launch is, too: all workgroups add up the cost of all units (request, key
 // head, tile of rows; cost = tiles of keys + a constant), and workgroup w takes the w-th of equal spans of that line.  A

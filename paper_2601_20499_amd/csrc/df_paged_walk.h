@@ -197,8 +197,8 @@ DF_WALK unsigned eight_keys(const Keys &x, int k) { return below8(x.a - k) | (be
 // The units' costs (tiles + a constant) form a line, requests outermost, then key heads, then tiles of rows (neighbours read the same keys); it is
 // cut into equal spans.
 // Cost of a unit besides its tiles, in tiles: its request, pages and queries are fetched one after the other, and its hidden tiles take longer than
-// others.  4, 10, 16, 24: single tokens 236, 206, 204, 206 us, prompt pieces 506, 471, 462, 495, 390-token frames 87, 77, 80, 79,
-// 480p chunks 640, 634, 643, 654.
+// others.  When it was set, 4, 10, 16, 24: single tokens 236, 206, 204, 206 us, prompt pieces 506, 471, 462, 495, 390-token frames 87, 77, 80, 79,
+// 480p chunks 640, 634, 643, 654; since then 13 and 16 make no difference to 60 drawn cases (0.2 %).
 constexpr int kUnitCost = 10;
 constexpr int kSnap = 3;               // no piece of a cut unit has fewer tiles ...
 constexpr int kMinSpan = 8;            // ... than fit into the shortest span; units of up to kMinSpan tiles are not cut
